@@ -37,6 +37,9 @@ extern "C" {
 #endif
 
 #define BEBOP_MAX_K 32   /* accept bits of one sequence fit one warp ballot */
+#define BEBOP_MAX_TOP 1024          /* teacher entries of a row (bebop_distill) */
+#define BEBOP_MAX_ROWS ((1 << 27) - 1)   /* rows or sequences of a call that takes no workspace */
+#define BEBOP_MAX_DISTILL_V (1 << 24)    /* vocabulary of bebop_distill */
 
 typedef enum {
     BEBOP_OK = 0,
@@ -48,7 +51,8 @@ typedef enum {
     BEBOP_ERR_TEMPERATURE = 6,
     BEBOP_ERR_ARCH = 7,
     BEBOP_ERR_CUDA = 8,
-    BEBOP_ERR_STATIC_SCRATCH = 9
+    BEBOP_ERR_STATIC_SCRATCH = 9,
+    BEBOP_ERR_OVERLAP = 10
 } bebop_status_t;
 
 typedef enum { BEBOP_F32 = 0, BEBOP_BF16 = 1 } bebop_dtype_t;
@@ -164,13 +168,77 @@ bebop_status_t bebop_greedy_verify(
     void* workspace, size_t workspace_bytes, void* cuda_stream);
 
 /*
+ * Target-only verification (Sec. 2.2, target-only sampling) of drafts that come without a distribution (argmax drafts,
+ * look-up drafts): for each sequence b with L = draft_len[b] drafts and p_k = softmax(target[b,k,:]/tau_b)
+ *   accept x_k while u_accept[b,k] < p_k(x_k); stop at the first reject
+ *   at a reject at position n: draw y from p_n without x_n, renormalised; if all L accepted: from p_L
+ *     y = min{ v : sum_{v'<=v} r(v') >= u_final[b] * sum r }
+ * so that every emitted token is distributed as the target's.  Rows behind the stop are never read, and no anomaly in them is seen.
+ * The accept test and the draw are decided as an fp64 evaluation decides them except on near-ties.
+ * Arguments as in bebop_verify; p_draft [B,K] (may be NULL): p_k(x_k) of the positions read, 0 behind the stop.
+ * BEBOP_ROW_ZERO_RESID: a draft of probability 1 was rejected (u_accept >= 1); the token is the draft.
+ * One launch, no workspace: calls on several streams may overlap.  B <= BEBOP_MAX_ROWS.
+ */
+bebop_status_t bebop_target_only_verify(
+    const void* target_logits, int64_t ld_target,
+    const int32_t* draft_tokens, const int32_t* draft_len,
+    const float* temperature, float temperature_all,
+    const float* u_accept, const float* u_final,
+    int B, int K, int V, bebop_dtype_t dt,
+    int32_t* accept_len, int32_t* out_tokens, float* p_draft, int32_t* row_status,
+    void* cuda_stream);
+
+/*
+ * The TV loss of N row pairs with its gradient in the draft logits (Eq. tv_grad; App. F, Algorithms 1 and 2, in one call):
+ *   tv[n] and s_aux[n] as in bebop_tv (each may be NULL)
+ *   grad_draft[n,v] = -(grad_tv[n] / tau_n) q(v) (1[q(v) <= p(v)] - s_aux[n])
+ * The comparison q(v) <= p(v), at which the gradient jumps, is the one of an fp64 evaluation.
+ * grad_tv [N] fp32: the loss's gradient in tv[n] (a mean's 1/N, 0 for a padded row), or NULL (= 1).
+ * grad_draft [N,V]: dtype dt, rounded once from fp32; rows as the logits' (ld_grad, alignment); what lies between V and ld_grad is
+ *   left as it is.  It must not share memory with the logits (BEBOP_ERR_OVERLAP).
+ * A row with a FATAL bit has gradient 0.  One launch, no workspace: calls on several streams may overlap.  N <= BEBOP_MAX_ROWS.
+ */
+bebop_status_t bebop_tv_grad(
+    const void* target_logits, int64_t ld_target,
+    const void* draft_logits, int64_t ld_draft,
+    const float* temperature, float temperature_all, const float* grad_tv,
+    int N, int V, bebop_dtype_t dt,
+    void* grad_draft, int64_t ld_grad, float* tv, float* s_aux, int32_t* row_status,
+    void* cuda_stream);
+
+/*
+ * Distillation from a teacher's top logits (the forward KL of the paper's training objectives, for a target whose rows are only
+ * kept as their T largest logits), with its gradient in the draft logits.  q = softmax(draft[n,:]/tau_n); an entry is a token id
+ * and the target's logit of it; id -1 is no entry (short lists).
+ *   target_lse NULL: p = softmax of the row's entries / tau;  loss = sum_i p_i (log p_i - log q_i)
+ *   target_lse [N]:  p_i = exp(t_i / tau - target_lse[n]), the logsumexp of the target's whole row / tau; the mass that the entries
+ *                    leave out, r = max(0, 1 - sum p_i), meets the draft's outside them, s: loss += r log(r / s)
+ *   grad_draft[n,v] = (grad_loss[n] / tau_n) ((P + r) q(v) - p(v)) for an entry, (grad_loss[n] / tau_n) (P + r - r/s) q(v) elsewhere, P = sum p_i
+ * The loss is +inf where the target gives mass to what the draft masks.  A row without entries (an ignored position) has loss 0,
+ * gradient 0 and status 0, whatever its logits.
+ * top_ids, top_logits [N,T], contiguous, 1 <= T <= BEBOP_MAX_TOP; top_logits of type top_dt; ids of a row in any order, each once
+ *   (an id given twice, below -1 or >= V: BEBOP_ROW_BAD_TOKEN).  V <= BEBOP_MAX_DISTILL_V, N <= BEBOP_MAX_ROWS.
+ * BEBOP_ROW_NONFINITE also for a NaN or +inf entry or target_lse (an infinite one), BEBOP_ROW_EMPTY also for entries that are all -inf where target_lse is NULL.
+ * grad_loss [N] or NULL (= 1); grad_draft as in bebop_tv_grad, or NULL (loss only); a row with a FATAL bit has loss 0, gradient 0.
+ * One launch, no workspace: calls on several streams may overlap.
+ */
+bebop_status_t bebop_distill(
+    const void* draft_logits, int64_t ld_draft,
+    const int32_t* top_ids, const void* top_logits, bebop_dtype_t top_dt, int T, const float* target_lse,
+    const float* temperature, float temperature_all, const float* grad_loss,
+    int N, int V, bebop_dtype_t dt,
+    float* loss, void* grad_draft, int64_t ld_grad, int32_t* row_status,
+    void* cuda_stream);
+
+/*
  * Test and measurement hooks (no counterpart in the paper).  They set process-wide switches that every later
  * call in the process sees: not thread-safe, and not meant for code that serves requests.
  * bebop_debug_force_general_path(mode) chooses the kernels behind bebop_verify, bebop_tv and bebop_greedy_verify:
  * 0 (the default) the fastest, by measurement, of the sequence, the fused and the pipelined kernel for the shape, and the
  * split-row general kernels for shapes none of them takes; 1 the general kernels always; 2 the pipelined kernel
  * wherever it applies; 3 the fused kernel wherever it applies (the greedy mode has no fused form); 4 the sequence kernel
- * wherever it applies.  All give the same results up to the documented tolerances.  bebop_debug_last_kernel() says
+ * wherever it applies.  All give the same results up to the documented tolerances.  (bebop_target_only_verify, bebop_tv_grad and
+ * bebop_distill: with 1 they read their rows from memory in every pass, as they do for rows that sixteen SMs cannot hold.)  bebop_debug_last_kernel() says
  * what the last of these calls ran: 1 the general kernels, 2 the pipelined kernel, 3 the fused or the sequence
  * kernel (0: no call yet); bebop_debug_last_kernel_name() says it by name: "general", "k_pipe" (its sweeps, or with a TV
  * output the stream, k_fuse, under this name), "k_fuse", "k_seq", "k_seq_greedy" ("none": no call yet).
@@ -181,7 +249,7 @@ bebop_status_t bebop_greedy_verify(
  * bebop_verify calls record around the main (pipelined or fused) kernel, on the caller's stream (NULL,
  * NULL switches it off).
  * bebop_debug_expire_wait(which): the next call's device-side wait number `which` (1: the re-draw kernel's wait
- * for the list of sequences; 2: the main kernel's wait for what other CTAs deliver) gives up at once, as if
+ * for the list of sequences; 2: the main kernel's wait for what other CTAs deliver; either: the three calls without a workspace) gives up at once, as if
  * its bound had run out: the call still returns, every row_status carries BEBOP_ROW_WAIT_EXPIRED, and the call
  * after it is normal again (0: off).  For the test of the bounded waits; nothing is trapped or hung.
  * bebop_debug_set_draw_kappa(kappa): the factor in the error bound that decides whether bebop_verify keeps a token

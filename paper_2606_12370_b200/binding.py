@@ -2,7 +2,8 @@
 
 Argument marshalling only: tensors are torch CUDA tensors whose device pointers
 are handed to the library, outputs are allocated when not supplied, and the
-call is enqueued on torch's current stream.  Nothing is computed here: the four
+call is enqueued on torch's current stream (the three calls without a workspace: the current
+stream of the logits' device, whichever device is current).  Nothing is computed here: the seven
 calls go through the native marshaller csrc/bebop_host.cpp (_bebop_host.so, built
 beside the library), everything else through ctypes.
 """
@@ -50,6 +51,12 @@ def load_library():
     lib.bebop_tv_static.argtypes = [vp, i64, vp, i64, vp, f32, i32, i32, i32, vp, vp, vp, vp]
     lib.bebop_greedy_verify.restype = i32
     lib.bebop_greedy_verify.argtypes = [vp, i64, vp, vp, i32, i32, i32, i32, vp, vp, vp, vp, sz, vp]
+    lib.bebop_target_only_verify.restype = i32
+    lib.bebop_target_only_verify.argtypes = [vp, i64, vp, vp, vp, f32, vp, vp, i32, i32, i32, i32, vp, vp, vp, vp, vp]
+    lib.bebop_tv_grad.restype = i32
+    lib.bebop_tv_grad.argtypes = [vp, i64, vp, i64, vp, f32, vp, i32, i32, i32, vp, i64, vp, vp, vp, vp]
+    lib.bebop_distill.restype = i32
+    lib.bebop_distill.argtypes = [vp, i64, vp, vp, i32, i32, vp, vp, f32, vp, i32, i32, i32, vp, vp, i64, vp, vp]
     lib.bebop_debug_force_general_path.restype = None
     lib.bebop_debug_force_general_path.argtypes = [i32]
     lib.bebop_debug_set_timing_events.restype = None
@@ -93,7 +100,8 @@ def _load_host():
         raise ImportError("_bebop_host.so is missing or does not load: build it with "
                           "`python -m paper_2606_12370_b200.build`") from e
     host.init(*(C.cast(f, C.c_void_p).value for f in
-                (lib.bebop_verify, lib.bebop_tv, lib.bebop_tv_static, lib.bebop_greedy_verify, lib.bebop_workspace_bytes)))
+                (lib.bebop_verify, lib.bebop_tv, lib.bebop_tv_static, lib.bebop_greedy_verify, lib.bebop_workspace_bytes,
+                 lib.bebop_target_only_verify, lib.bebop_tv_grad, lib.bebop_distill)))
     _host = host
     return host
 
@@ -180,3 +188,35 @@ def bebop_tv_static(target_logits, draft_logits, temperature=None, temperature_a
 def bebop_greedy_verify(target_logits, draft_tokens, draft_len=None, workspace=None):
     """Greedy-draft mode: accept while x_k equals the target argmax."""
     return _result((_host or _load_host()).greedy_verify(target_logits, draft_tokens, draft_len, workspace, POISON_OUTPUTS))
+
+
+def _dict_or_none(out):
+    return None if not out else out if isinstance(out, dict) else dict(out)
+
+
+def bebop_target_only_verify(target_logits, draft_tokens, u_accept, u_final, draft_len=None, temperature=None, temperature_all=1.0,
+                             out=None, want_probs=True, want_status=True):
+    """Verification of drafts that come without a distribution (argmax drafts, look-up drafts): accept while u < p(x), else draw
+    from p without the draft.  Returns a dict of CUDA tensors: accept_len [B] i32, out_tokens [B,K+1] i32, p_draft [B,K] f32
+    (0 behind the stop), row_status [B] i32 (the last two None when not requested).  `out`: buffers for any of them."""
+    return _result((_host or _load_host()).target_only_verify(target_logits, draft_tokens, u_accept, u_final, draft_len, temperature, temperature_all,
+                                                              _dict_or_none(out), want_probs, want_status, POISON_OUTPUTS))
+
+
+def bebop_tv_grad(target_logits, draft_logits, temperature=None, temperature_all=1.0, grad_tv=None, out=None,
+                  want_tv=True, want_s_aux=True, want_status=True):
+    """The TV loss of N row pairs [N,V] with its gradient in the draft logits, in one call: grad_draft [N,V] of the logits' type,
+    tv and s_aux [N] f32, row_status [N] i32.  grad_tv [N] f32: the gradient of the loss in tv (None: 1).  To train:
+    `draft_logits.backward(r["grad_draft"])`.  `out`: buffers for any of them (grad_draft's rows on 16-byte boundaries)."""
+    return _result((_host or _load_host()).tv_grad(target_logits, draft_logits, temperature, temperature_all, grad_tv, _dict_or_none(out),
+                                                   want_tv, want_s_aux, want_status, POISON_OUTPUTS))
+
+
+def bebop_distill(draft_logits, top_ids, top_logits, target_lse=None, temperature=None, temperature_all=1.0, grad_loss=None, out=None,
+                  want_grad=True, want_status=True):
+    """KL divergence of the draft's rows [N,V] from a target of which T logits a row are kept: top_ids [N,T] i32 (-1: no entry) and
+    top_logits [N,T] f32 or bf16.  target_lse [N] f32, the logsumexp of the target's whole rows / temperature, makes what the entries
+    leave out count; without it they are the whole target.  Returns loss [N] f32, grad_draft [N,V] of the logits' type (times
+    grad_loss [N] f32, None: 1; None when not requested), row_status [N] i32.  `out`: buffers for any of them."""
+    return _result((_host or _load_host()).distill(draft_logits, top_ids, top_logits, target_lse, temperature, temperature_all, grad_loss,
+                                                   _dict_or_none(out), want_grad, want_status, POISON_OUTPUTS))

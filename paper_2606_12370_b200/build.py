@@ -11,7 +11,7 @@ LIB = os.path.join(HERE, "libbebop.so")
 HOST = os.path.join(HERE, "_bebop_host.so")
 HOST_FOR = HOST + ".for"       # the versions it was made for
 SOURCES = ["bebop_api.cu", "bebop_general.cu", "bebop_redraw.cu", "bebop_pipe.cu", "bebop_fuse.cu",
-           "bebop_seq.cu"]
+           "bebop_seq.cu", "bebop_tonly.cu", "bebop_tvgrad.cu", "bebop_distill.cu"]
 NVCC = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
 FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
          "-Xcompiler", "-fPIC", "-shared"]

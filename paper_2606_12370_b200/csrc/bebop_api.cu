@@ -73,6 +73,21 @@ RowArgs row_args(const void* target, int64_t ld_t, const void* draft, int64_t ld
     return a;
 }
 
+// What the calls without a workspace need of a plan: 16-byte vectors per row.
+Plan whole_rows(int V, bebop_dtype_t dt) {
+    Plan p = {};
+    const int vec = dt == BEBOP_F32 ? 4 : 8;
+    p.nvec = (V + vec - 1) / vec; p.nsplit = 1;
+    return p;
+}
+
+// Whether two sets of N rows share bytes, from the first row's start to the last row's end.
+bool rows_overlap(const void* x, int64_t ldx, const void* y, int64_t ldy, int N, int V, bebop_dtype_t dt) {
+    const uintptr_t es = dt == BEBOP_F32 ? 4 : 2, a = reinterpret_cast<uintptr_t>(x), b = reinterpret_cast<uintptr_t>(y);
+    const uintptr_t na = ((uintptr_t)(N - 1) * (uintptr_t)ldx + (uintptr_t)V) * es, nb = ((uintptr_t)(N - 1) * (uintptr_t)ldy + (uintptr_t)V) * es;
+    return a < b + nb && b < a + na;
+}
+
 }  // namespace
 
 namespace bebop {
@@ -232,6 +247,60 @@ bebop_status_t bebop_tv_static(const void* target_logits, int64_t ld_target, con
     return e == cudaSuccess ? BEBOP_OK : BEBOP_ERR_CUDA;
 }
 
+bebop_status_t bebop_target_only_verify(const void* target_logits, int64_t ld_target, const int32_t* draft_tokens, const int32_t* draft_len,
+                                        const float* temperature, float temperature_all, const float* u_accept, const float* u_final, int B, int K,
+                                        int V, bebop_dtype_t dt, int32_t* accept_len, int32_t* out_tokens, float* p_draft, int32_t* row_status,
+                                        void* cuda_stream) {
+    bebop_status_t s = check_shape(B, K, V, dt);
+    if (s != BEBOP_OK) return s;
+    if (B > BEBOP_MAX_ROWS) return BEBOP_ERR_SHAPE;
+    if (!draft_tokens || !u_accept || !u_final || !accept_len || !out_tokens) return BEBOP_ERR_NULL;
+    if ((s = check_rows(target_logits, ld_target, V, dt)) != BEBOP_OK) return s;
+    if (!temperature && !(temperature_all > 0.f && temperature_all < INFINITY)) return BEBOP_ERR_TEMPERATURE;
+    if ((s = check_arch()) != BEBOP_OK) return s;
+    const RowArgs a = row_args(target_logits, ld_target, nullptr, 0, K + 1, K, draft_len, temperature, temperature_all, B, K, V, dt, whole_rows(V, dt));
+    const cudaError_t e = target_only(a, draft_tokens, u_accept, u_final, accept_len, out_tokens, p_draft, row_status, g_path == 1,
+                                      static_cast<cudaStream_t>(cuda_stream));
+    return e == cudaSuccess ? BEBOP_OK : BEBOP_ERR_CUDA;
+}
+
+bebop_status_t bebop_tv_grad(const void* target_logits, int64_t ld_target, const void* draft_logits, int64_t ld_draft, const float* temperature,
+                             float temperature_all, const float* grad_tv, int N, int V, bebop_dtype_t dt, void* grad_draft, int64_t ld_grad,
+                             float* tv, float* s_aux, int32_t* row_status, void* cuda_stream) {
+    bebop_status_t s = check_shape(N, 1, V, dt);
+    if (s != BEBOP_OK) return s;
+    if (N > BEBOP_MAX_ROWS) return BEBOP_ERR_SHAPE;
+    if ((s = check_rows(target_logits, ld_target, V, dt)) != BEBOP_OK) return s;
+    if ((s = check_rows(draft_logits, ld_draft, V, dt)) != BEBOP_OK) return s;
+    if ((s = check_rows(grad_draft, ld_grad, V, dt)) != BEBOP_OK) return s;
+    if (!temperature && !(temperature_all > 0.f && temperature_all < INFINITY)) return BEBOP_ERR_TEMPERATURE;
+    if (rows_overlap(grad_draft, ld_grad, target_logits, ld_target, N, V, dt) || rows_overlap(grad_draft, ld_grad, draft_logits, ld_draft, N, V, dt))
+        return BEBOP_ERR_OVERLAP;
+    if ((s = check_arch()) != BEBOP_OK) return s;
+    const RowArgs a = row_args(target_logits, ld_target, draft_logits, ld_draft, 1, 1, nullptr, temperature, temperature_all, N, 1, V, dt, whole_rows(V, dt));
+    const cudaError_t e = tv_grad(a, grad_tv, tv, s_aux, row_status, grad_draft, ld_grad, g_path == 1, static_cast<cudaStream_t>(cuda_stream));
+    return e == cudaSuccess ? BEBOP_OK : BEBOP_ERR_CUDA;
+}
+
+bebop_status_t bebop_distill(const void* draft_logits, int64_t ld_draft, const int32_t* top_ids, const void* top_logits, bebop_dtype_t top_dt, int T,
+                             const float* target_lse, const float* temperature, float temperature_all, const float* grad_loss, int N, int V,
+                             bebop_dtype_t dt, float* loss, void* grad_draft, int64_t ld_grad, int32_t* row_status, void* cuda_stream) {
+    bebop_status_t s = check_shape(N, 1, V, dt);
+    if (s != BEBOP_OK) return s;
+    if (top_dt != BEBOP_F32 && top_dt != BEBOP_BF16) return BEBOP_ERR_DTYPE;
+    if (N > BEBOP_MAX_ROWS || V > BEBOP_MAX_DISTILL_V || T < 1 || T > BEBOP_MAX_TOP) return BEBOP_ERR_SHAPE;
+    if (!top_ids || !top_logits || !loss) return BEBOP_ERR_NULL;
+    if ((s = check_rows(draft_logits, ld_draft, V, dt)) != BEBOP_OK) return s;
+    if (grad_draft && (s = check_rows(grad_draft, ld_grad, V, dt)) != BEBOP_OK) return s;
+    if (!temperature && !(temperature_all > 0.f && temperature_all < INFINITY)) return BEBOP_ERR_TEMPERATURE;
+    if (grad_draft && rows_overlap(grad_draft, ld_grad, draft_logits, ld_draft, N, V, dt)) return BEBOP_ERR_OVERLAP;
+    if ((s = check_arch()) != BEBOP_OK) return s;
+    const RowArgs a = row_args(nullptr, 0, draft_logits, ld_draft, 1, 1, nullptr, temperature, temperature_all, N, 1, V, dt, whole_rows(V, dt));
+    const cudaError_t e = distill(a, top_ids, top_logits, (int)top_dt, T, target_lse, grad_loss, loss, row_status, grad_draft, ld_grad, g_path == 1,
+                                  static_cast<cudaStream_t>(cuda_stream));
+    return e == cudaSuccess ? BEBOP_OK : BEBOP_ERR_CUDA;
+}
+
 void bebop_debug_force_general_path(int on) { g_path = on; }
 
 int bebop_debug_last_kernel(void) { return g_last.id; }
@@ -253,7 +322,7 @@ const char* bebop_status_string(bebop_status_t status) {
     switch (status) {
         case BEBOP_OK: return "ok";
         case BEBOP_ERR_NULL: return "a required pointer is NULL";
-        case BEBOP_ERR_SHAPE: return "bad shape: need B, K, V > 0, K <= 32, ld >= V";
+        case BEBOP_ERR_SHAPE: return "bad shape: need B, K, V > 0, K <= 32, ld >= V, and what the call's own limits say";
         case BEBOP_ERR_DTYPE: return "unknown dtype";
         case BEBOP_ERR_ALIGN: return "logit rows must be 16-byte aligned, workspace 256-byte aligned";
         case BEBOP_ERR_WORKSPACE: return "workspace smaller than bebop_workspace_bytes()";
@@ -262,6 +331,7 @@ const char* bebop_status_string(bebop_status_t status) {
         case BEBOP_ERR_CUDA: return "CUDA launch error";
         case BEBOP_ERR_STATIC_SCRATCH:
             return "shape needs more than the built-in scratch of bebop_tv_static: use bebop_tv with a workspace";
+        case BEBOP_ERR_OVERLAP: return "the gradient shares memory with the logits";
     }
     return "unknown status";
 }

@@ -1,0 +1,216 @@
+// What the kernels that take a row (a row pair) by a cluster of CTAs and need no other launch share: the slice of a row that a
+// CTA holds, its softmax sums around float references, the exchange of the CTAs' sums, the launch.
+//
+// A softmax sum here is (m, s) with s = sum 2^((x - m) c), c = log2(e) / tau as two floats.  The difference x - m comes first, so
+// rows of any finite size are evaluated as defined: a row of nothing but a mask of -1e9, or of the type's lowest value, gives
+// equal weights.  (The kernels with integer exponents save an addition per two logits by fma(x, c, -E) and need a bound on |x c|.)
+// m is a reference, not the maximum: a warp keeps its first chunk's and moves it only when a chunk lies 2^16 above it, so that its
+// running sum is hardly ever rescaled.
+#pragma once
+#include "bebop_chunk.cuh"
+
+namespace bebop {
+
+namespace {
+
+constexpr int RV = 4;                         // vectors per lane of a chunk
+constexpr int RCV = 32 * RV;                  // vectors per chunk
+constexpr int kRowsMaxCluster = 16;
+constexpr int kRowsMaxWarps = 16;
+constexpr int kRowsSmem = 232448 - 4096;      // dynamic shared memory of a CTA, at most (the rest: static tables)
+constexpr uint32_t kRowsSpin = 1u << 24;
+constexpr float kRowsSlack = 16.f;            // a sum's terms are at most 2^kRowsSlack
+
+// log2(e) / tau, finite whatever tau, so that 0 * c is 0: to double precision (d), as the nearest float (c), and as a sum of floats hi + lo with lo
+// above 0, so that a masked logit's -inf stays -inf in both products.
+struct RScale { double d; float c, hi, lo, slack; };      // slack: kRowsSlack in units of logits
+__device__ __forceinline__ RScale rows_scale(float tau) {
+    RScale r;
+    r.d = fmin(1.4426950408889634 / (tau_ok(tau) ? (double)tau : 1.0), 3e38);
+    r.c = (float)r.d;
+    r.hi = __int_as_float(__float_as_int(__double2float_rd(r.d)) - 1);
+    r.lo = fmaxf((float)(r.d - (double)r.hi), 1e-45f);
+    r.slack = (float)((double)kRowsSlack / r.d);
+    return r;
+}
+
+struct __align__(16) RSum { double s; float m; int bad; };      // bad: bit 0 a NaN or +inf, bit 1 a wait that gave up
+__device__ __forceinline__ RSum no_sum() { RSum r; r.s = 0.0; r.m = -INFINITY; r.bad = 0; return r; }
+
+// The slice of a row: vectors [v0, v0 + nv) of it, in shared memory (RES) or where the caller has them.
+struct Slice { const unsigned char* p; int v0, nv, V; };
+
+// vector vi of a slice; what lies beyond the slice or the vocabulary reads as -inf
+template <int DT, bool RES>
+__device__ __forceinline__ uint4 row_vec(const Slice& s, int vi) {
+    constexpr int VEC = Elem<DT>::VEC;
+    uint4 x = neg_inf_vec<DT>();
+    if (vi < s.nv) {
+        x = RES ? *reinterpret_cast<const uint4*>(s.p + (size_t)vi * 16) : ldg16_stream(s.p + (size_t)vi * 16);
+        const int left = s.V - (s.v0 + vi) * VEC;
+        if (left < VEC) mask_tail<DT>(x, left);
+    }
+    return x;
+}
+
+// x - m of a vector's logits, and their scaled differences' exponentials, two at a time.  bf16 logits: the low part of c is
+// below what the result is rounded to.
+template <int DT, bool LOW>
+__device__ __forceinline__ void row_exp(const uint4& raw, float m, const RScale& c, float* e) {
+    constexpr int VEC = Elem<DT>::VEC;
+    float f[VEC];
+    unpack<DT>(raw, f);
+    const float2 m2 = make_float2(-m, -m), c2 = LOW ? make_float2(c.hi, c.hi) : make_float2(c.c, c.c), l2 = make_float2(c.lo, c.lo);
+#pragma unroll
+    for (int i = 0; i < VEC; i += 2) {
+        const float2 d = __fadd2_rn(make_float2(f[i], f[i + 1]), m2);
+        float2 t = __fmul2_rn(d, c2);
+        if (LOW) t = __ffma2_rn(d, l2, t);
+        e[i] = ex2f(t.x);
+        e[i + 1] = ex2f(t.y);
+    }
+}
+
+// (a - b) 2^.. of two references, exactly enough: 2^((a - b) c), 0 where a is -inf
+__device__ __forceinline__ double ref_factor(float a, float b, double c) { return a == -INFINITY ? 0.0 : exp2(fmax(((double)a - (double)b) * c, -1100.0)); }
+
+// Sums of lanes [0, n) merged over a warp (the same bits in every lane).
+__device__ __forceinline__ RSum warp_merge(RSum r, double c) {
+    const int om = redux_max(f2ord(r.m));
+    RSum o;
+    o.m = ord2f(om);
+    o.bad = __reduce_or_sync(0xffffffffu, r.bad);
+    o.s = warp_sum(r.s * ref_factor(r.m, o.m, c));
+    return o;
+}
+
+// A warp's sum over vectors [a, b) of a slice: the lanes' parts in double, not yet added over the warp (s differs by lane).
+template <int DT, bool RES, bool LOW>
+__device__ __forceinline__ RSum warp_row_sum(const Slice& sl, int a, int b, const RScale& c) {
+    constexpr int VEC = Elem<DT>::VEC;
+    const int lane = threadIdx.x & 31;
+    RSum r = no_sum();
+    for (int v = a; v < b; v += RCV) {
+        uint4 x[RV];
+#pragma unroll
+        for (int j = 0; j < RV; ++j) { const int vi = v + j * 32 + lane; x[j] = vi < b ? row_vec<DT, RES>(sl, vi) : neg_inf_vec<DT>(); }
+        const float wm = ord2f(redux_max(f2ord(vecs_max<DT, RV>(x))));
+        if (!(wm < INFINITY)) { r.bad = 1; continue; }
+        if (wm == -INFINITY) continue;
+        if (!(wm <= r.m + c.slack)) {                          // (also: the first chunk with a logit)
+            r.s *= ref_factor(r.m, wm, c.d);
+            r.m = wm;
+        }
+        float2 s0 = make_float2(0.f, 0.f);
+#pragma unroll
+        for (int j = 0; j < RV; ++j) {
+            float e[VEC];
+            row_exp<DT, LOW>(x[j], r.m, c, e);
+#pragma unroll
+            for (int q = 0; q < VEC; q += 2) s0 = __fadd2_rn(s0, make_float2(e[q], e[q + 1]));
+        }
+        r.s += (double)(s0.x + s0.y);
+    }
+    return r;
+}
+
+// the warp's sum, added over its lanes
+__device__ __forceinline__ RSum warp_total(RSum r) { r.s = warp_sum(r.s); return r; }
+
+__device__ __forceinline__ void send_sum(RSum* at, const RSum& r, int rank) {
+    const uint32_t d = at_rank(at, rank);
+    st_remote(d, r.s); st_remote(d + 8, __float_as_int(r.m)); st_remote(d + 12, r.bad);
+}
+
+__device__ __forceinline__ int sum_status(const RSum& r) {
+    if (r.bad & 2) return ST_WAIT;
+    if ((r.bad & 1) || !(r.s == r.s)) return ST_NONFINITE;
+    return r.m == -INFINITY ? ST_EMPTY : 0;
+}
+
+__device__ __forceinline__ bool rows_wait(unsigned long long* b, uint32_t parity) {
+    const uint32_t addr = smem_u32(b);
+    for (uint32_t i = 0; i < kRowsSpin; ++i) if (mbar_try(addr, parity)) return true;
+    return false;
+}
+
+// gradient vector `vi` of a row (in its own type) from floats; a vector that ends beyond the vocabulary by its elements
+template <int DT>
+__device__ __forceinline__ void store_vec(unsigned char* row, int vi, int V, const float* f) {
+    constexpr int VEC = Elem<DT>::VEC;
+    const int left = V - vi * VEC;
+    if (left >= VEC) {
+        const uint4 x = pack<DT>(f);
+        asm volatile("st.global.cs.v4.u32 [%0], {%1,%2,%3,%4};" :: "l"(row + (size_t)vi * 16), "r"(x.x), "r"(x.y), "r"(x.z), "r"(x.w) : "memory");
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) if (i < left) {
+        if (DT == 0) reinterpret_cast<float*>(row)[(size_t)vi * VEC + i] = f[i];
+        else reinterpret_cast<unsigned short*>(row)[(size_t)vi * VEC + i] = (unsigned short)(pack_bf16x2(f[i], 0.f) & 0xffffu);
+    }
+}
+
+// ------------------------------------------------------------------ host
+struct RowsShape { int C, sv, bytes, threads; bool res; };      // CTAs per row, vectors per slice, dynamic shared memory, threads
+
+int rows_sms() {
+    static int cached[64] = {0};
+    int dev = 0, n = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess) return 0;
+    if (dev >= 0 && dev < 64 && cached[dev]) return cached[dev];
+    if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) { cudaGetLastError(); return 0; }
+    if (dev >= 0 && dev < 64) cached[dev] = n;
+    return n;
+}
+template <auto kernel> cudaError_t rows_ready() {
+    static bool done[64] = {false};
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    if (dev >= 0 && dev < 64 && done[dev]) return cudaSuccess;
+    if ((e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kRowsSmem)) != cudaSuccess) return e;
+    if ((e = cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1)) != cudaSuccess) return e;
+    if (dev >= 0 && dev < 64) done[dev] = true;
+    return cudaSuccess;
+}
+template <auto kernel, typename A> cudaError_t rows_launch(const A& args, int rows, const RowsShape& s, cudaStream_t stream) {
+    cudaError_t e = rows_ready<kernel>();
+    if (e != cudaSuccess) return e;
+    cudaLaunchAttribute attr[2];
+    attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[1].val.programmaticStreamSerializationAllowed = 1;
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = s.C; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)rows * (unsigned)s.C); cfg.blockDim = dim3(s.threads); cfg.dynamicSmemBytes = s.bytes; cfg.stream = stream;
+    cfg.attrs = s.C == 1 ? attr + 1 : attr; cfg.numAttrs = s.C == 1 ? 1 : 2;      // (a plain grid starts sooner than one of clusters)
+    return cudaLaunchKernelEx(&cfg, kernel, args);
+}
+
+// How a call's rows are cut: `held` row slices of a CTA side by side in shared memory, or, where sixteen CTAs cannot hold a row (or `stream` asks for
+// it), read from memory by every pass.  `extra` bytes and `bits` bits per vector are needed beside them.
+RowsShape rows_shape(int rows, int held, int nvec, bool stream, int extra = 0, int bits = 0) {
+    RowsShape s;
+    const int sms = rows_sms() > 0 ? rows_sms() : 148;
+    const auto slice = [&](int C) { return (nvec + C - 1) / C; };
+    const auto bytes = [&](int C) { return (long long)held * slice(C) * 16 + extra + (long long)slice(C) * bits / 8 + 8; };
+    s.res = !stream && bytes(kRowsMaxCluster) <= kRowsSmem;
+    s.C = kRowsMaxCluster;
+    if (s.res) {
+        const int share = 72000;
+        s.C = 1;
+        while (s.C < kRowsMaxCluster && bytes(s.C) > share) ++s.C;
+        while (s.C < kRowsMaxCluster && (long long)rows * (s.C + 1) <= sms && (long long)held * nvec > (long long)s.C * 2048) ++s.C;
+    }
+    s.sv = slice(s.C);
+    s.bytes = s.res ? held * s.sv * 16 : 0;
+    int warps = (int)(((long long)held * s.sv + RCV - 1) / RCV);
+    warps = warps < 4 ? 4 : warps > 8 ? 8 : warps;
+    s.threads = 32 * warps;
+    return s;
+}
+
+}  // namespace
+
+}  // namespace bebop
