@@ -101,8 +101,8 @@ def tv_grad(target, draft, grad_tv=None, temperature=None, temperature_all=1.0):
         # q <= p by the difference of the logits: the softmax's own rounding stays out of it
         zp, zq = target[i].astype(np.float64), draft[i].astype(np.float64)
         with np.errstate(invalid="ignore"):
-            theta = (zp.max() - zq.max()) + tau * (lq.max() - lp.max())
-            d = zp - zq
+            theta = tau * (lq.max() - lp.max())
+            d = (zp - zp.max()) - (zq - zq.max())
         below = np.where(q > 0, d >= theta, True)
         o["near"][i] = np.abs(np.where(q > 0, d - theta, np.inf)).min()
         o["tv"][i] = min(1.0, max(0.0, 0.5 * math.fsum(np.abs(p - q))))

@@ -33,34 +33,48 @@ struct DistillArgs {
     int expire;
 };
 
-// What a warp, a CTA and the cluster know of a row: the sum outside the entries, the entries' sum, W = sum w, A = sum w (t - t_max) / tau,
-// B = sum w (z - top_m) / tau, with w = exp((t - t_max) / tau).
-struct __align__(16) DSum { double s, top_s, W, A, B; float m, top_m; int bad, pad; };      // bad: 1 NaN or +inf, 2 wait, 4 bad id
+// What a warp knows of a row: the sum outside the entries, around m; of the entries the sum, around top_m (a logit), W = sum w, A = sum w (t_max - t) / tau,
+// B = sum w (top_m - z) / tau, with w = exp((t - t_max) / tau).
+struct __align__(16) DSum { double s, top_s, W, A, B; float m, top_m; int bad, pad; };      // bad: 1 NaN or +inf, 2 wait, 4 bad id, 8 an entry with weight that the draft masks
 
 __device__ __forceinline__ DSum no_dsum() {
     DSum d; d.s = d.top_s = d.W = d.A = d.B = 0.0; d.m = d.top_m = -INFINITY; d.bad = d.pad = 0;
     return d;
 }
-// W (a - b) / tau, also where nothing (W = 0) hangs on a
-__device__ __forceinline__ double moved(double W, float a, float b, double inv_tau) { return W > 0.0 && a != b ? W * (((double)a - (double)b) * inv_tau) : 0.0; }
-
-// sums of the lanes merged over a warp (the same bits in every lane)
-__device__ __forceinline__ DSum warp_merge(DSum d, double c, double inv_tau) {
-    DSum o;
-    o.m = ord2f(redux_max(f2ord(d.m)));
-    o.top_m = ord2f(redux_max(f2ord(d.top_m)));
-    o.bad = __reduce_or_sync(0xffffffffu, d.bad);
-    o.pad = 0;
-    o.s = warp_sum(d.s * ref_factor(d.m, o.m, c));
-    o.top_s = warp_sum(d.top_s * ref_factor(d.top_m, o.top_m, c));
-    o.W = warp_sum(d.W);
-    o.A = warp_sum(d.A);
-    o.B = warp_sum(d.B + moved(d.W, d.top_m, o.top_m, inv_tau));
+// 2^((a - b) c) of two logits, 0 where a is -inf
+__device__ __forceinline__ double logit_factor(float a, float b, const RScale& c) { return a == -INFINITY ? 0.0 : a == b ? 1.0 : q_exp2(((double)a - (double)b) * c.d, g_pow2_64); }
+// the entries' sums of `x` around the reference of `o`
+__device__ __forceinline__ void entries_into(DSum& o, const DSum& x, const RScale& c, double inv_tau) {
+    if (x.top_m == -INFINITY) { o.W += x.W; o.A += x.A; return; }
+    o.top_s += x.top_s * logit_factor(x.top_m, o.top_m, c);
+    o.W += x.W; o.A += x.A;
+    o.B += x.B + x.W * (((double)o.top_m - (double)x.top_m) * inv_tau);
+}
+// n warps' sums merged (the same bits in every lane)
+template <bool FAR> __device__ __forceinline__ DSum warp_merge(const DSum* s, int n, const RScale& c, double inv_tau) {
+    const int lane = threadIdx.x & 31;
+    float m = -INFINITY, tm = -INFINITY;
+    int bad = 0;
+    for (int i = lane; i < n; i += 32) { m = fmaxf(m, s[i].m); tm = fmaxf(tm, s[i].top_m); bad |= s[i].bad; }
+    DSum o = no_dsum();
+    o.m = ord2f(redux_max(f2ord(m)));
+    o.top_m = ord2f(redux_max(f2ord(tm)));
+    for (int i = lane; i < n; i += 32) {
+        o.s += s[i].s * ref_factor<FAR>(s[i].m, o.m, c);
+        if (s[i].W > 0.0 || s[i].top_m > -INFINITY) entries_into(o, s[i], c, inv_tau);
+    }
+    o.bad = __reduce_or_sync(0xffffffffu, bad);
+    o.s = warp_sum_pos(o.s);
+    o.top_s = warp_sum(o.top_s); o.W = warp_sum(o.W); o.A = warp_sum(o.A); o.B = warp_sum(o.B);      // (in double: 1 - P is what matters of W, and B may be as large as a logit)
     return o;
 }
 
+// What the gradient needs: (g / tau) / sum q (P + r), (g / tau) k, the factor outside the entries, the reference; the row has none; it is to be done again as FAR.
+struct DistillGrad { double q, w; float other, M; int nothing, far; };
+
 struct DistillShared {
-    DSum warp[kRowsMaxWarps], cta[kRowsMaxCluster];
+    DSum sum[kRowsMaxParts];  // the warps' sums of all CTAs, by rank and warp
+    DistillGrad grad;
     unsigned long long bar[kRowsMaxWarps];
 };
 
@@ -80,10 +94,165 @@ template <int DT> __device__ __forceinline__ uint4 without_entries(uint4 x, uint
     return pack<DT>(f);
 }
 
+// What a warp brings to the passes over the row.
+struct DistillRow {
+    Slice sl;
+    uint32_t* bits;
+    float* ez;
+    double* ew;
+    const int32_t* ids;
+    RScale c;
+    double inv_tau;
+    float tau, lse;
+    DSum d;                   // the entries' sums
+    int bad, valid, rank, b, wa, wb, v0, t0, t1;
+    float tmax;
+};
+
+// The row's numbers from the merged sums.
+struct DistillNumbers { float M; double up, tail, total, logk, k, P, r; int st, nothing, far; };
+template <bool FAR> __device__ __forceinline__ DistillNumbers numbers(const DistillArgs& a, const DistillRow& w, const DSum& d) {
+    const RScale& c = w.c;
+    DistillNumbers o;
+    o.far = !FAR && !(d.bad & 7) && w.valid && tau_ok(w.tau) && (sum_far(d.m) || (fabs((double)d.top_m * c.d) >= (double)kRowsFar && d.top_m > -INFINITY));
+    // both sums around M
+    o.M = fmaxf(d.m, FAR ? d.top_m : (float)((double)d.top_m * c.d));
+    o.up = d.top_m == -INFINITY ? 0.0 : row_arg<FAR>(d.top_m, o.M, c);      // the entries' reference above M, as a power of two
+    o.tail = d.m == -INFINITY ? 0.0 : d.s * q_exp2(FAR ? ((double)d.m - (double)o.M) * c.d : (double)d.m - (double)o.M, g_pow2_64);
+    o.total = o.tail + (d.top_m == -INFINITY ? 0.0 : d.top_s * q_exp2(o.up, g_pow2_64));
+    o.st = 0;
+    if (d.bad & 2) o.st = ST_WAIT;
+    else if (!tau_ok(w.tau)) o.st = ST_BAD_TEMP;
+    else if (d.bad & 4) o.st = ST_BAD_TOKEN;
+    else if (w.valid) o.st = d.bad & 1 ? ST_NONFINITE : o.M == -INFINITY || (!a.lse && !(d.W > 0.0)) ? ST_EMPTY : 0;
+    o.nothing = o.st != 0 || !w.valid;
+    o.logk = a.lse ? (double)w.tmax * w.inv_tau - (double)w.lse : 0.0;
+    o.k = a.lse ? (d.W > 0.0 ? q_exp2(fmin(o.logk * 1.4426950408889634, 1000.0), g_pow2_64) : 0.0) : 1.0 / d.W;
+    o.P = a.lse ? o.k * d.W : 1.0;
+    o.r = a.lse ? fmax(1.0 - o.P, 0.0) : 0.0;
+    return o;
+}
+// KL: sum p (log p - log q) + r log(r / s).  (Of rank 0, behind the gradient: its logarithms are on nobody's way there.)
+__device__ __forceinline__ double kl(const DistillArgs& a, const DSum& d, const DistillNumbers& o) {
+    // the entries' logits lie B / W below top_m in the mean, which lies `up` above M
+    const double logS = log(o.total), logk = a.lse ? o.logk : -log(d.W);
+    double loss = 0.0;
+    if (d.W > 0.0) loss = o.P * (logk + logS) - o.k * (d.A - d.B + d.W * (o.up * 0.6931471805599453));
+    if (o.r > 0.0) loss += o.r * (log(o.r) - log(o.tail) + logS);
+    return d.bad & 8 ? INFINITY : loss;
+}
+
+template <int DT, bool RES, bool FAR> __device__ __forceinline__ void gradient(const DistillArgs& a, const DistillRow& w, const DistillGrad& g) {
+    constexpr int VEC = Elem<DT>::VEC;
+    const RowArgs& R = a.r;
+    const RScale& c = w.c;
+    const int lane = threadIdx.x & 31;
+    unsigned char* const grow = a.grad + (int64_t)w.b * a.g_row_bytes;
+    if (g.nothing) {
+        float z[VEC];
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) z[i] = 0.f;
+        for (int v = w.wa + lane; v < w.wb; v += 32) store_vec<DT>(grow, w.v0 + v, R.V, z);
+        return;
+    }
+    int v = w.wa + lane;
+    if (RES && !FAR) {
+        const int full = min(w.wb, R.V / VEC - w.v0);
+#pragma unroll 2
+        for (; v < full; v += 32) {
+            float e[VEC];
+            row_exp<DT, DT == 0, FAR>(*reinterpret_cast<const uint4*>(w.sl.p + (size_t)v * 16), g.M, c, e);
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) e[i] *= g.other;
+            store_whole<DT>(grow, w.v0 + v, e);
+        }
+    }
+    for (; v < w.wb; v += 32) {
+        float e[VEC];
+        uint4 x = row_vec<DT, RES>(w.sl, v);
+        if (!RES) x = without_entries<DT>(x, entry_bits<DT>(w.bits, v));
+        row_exp<DT, DT == 0, FAR>(x, g.M, c, e);
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) e[i] *= g.other;
+        store_vec<DT>(grow, w.v0 + v, R.V, e);
+    }
+    __syncwarp();                                           // (the warp's entries, behind the vectors that hold them)
+    for (int i = lane; i < a.T; i += 32) {
+        const int id = w.ids[i];
+        if (id < w.t0 || id >= w.t1) continue;
+        const double q = w.ez[i] > -INFINITY ? q_exp2(row_arg<FAR>(w.ez[i], g.M, c), g_pow2_64) : 0.0;
+        const float x = (float)(g.q * q - g.w * w.ew[i]);
+        if (DT == 0) reinterpret_cast<float*>(grow)[id] = x;
+        else reinterpret_cast<unsigned short*>(grow)[id] = (unsigned short)(pack_bf16x2(x, 0.f) & 0xffffu);
+    }
+}
+// The sum outside the entries, the exchange, the loss and the gradient.  True: the row is FAR, and nothing has been written.
+template <int DT, bool RES, bool FAR>
+__device__ __forceinline__ bool distill_rest(const DistillArgs& a, DistillShared& S, const DistillRow& w, bool first) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, nw = blockDim.x >> 5, C = a.s.C;
+    const RScale& c = w.c;
+    const double inv_tau = w.inv_tau;
+    DSum d = w.d;
+    d.bad = w.bad;
+    // ---- pass 1
+    if (RES) {
+        const RSum r = warp_row_sum<DT, true, true, FAR>(w.sl, w.wa, w.wb, c);
+        d.s = r.s; d.m = r.m; d.bad |= r.bad;
+    } else {
+        RSum r = no_sum();
+        for (int v = w.wa; v < w.wb; v += RCV) {
+            uint4 x[RV];
+#pragma unroll
+            for (int j = 0; j < RV; ++j) {
+                const int vi = v + j * 32 + lane;
+                x[j] = vi < w.wb ? without_entries<DT>(row_vec<DT, false>(w.sl, vi), entry_bits<DT>(w.bits, vi)) : neg_inf_vec<DT>();
+            }
+            chunk_into<DT, true, FAR>(r, x, c);
+        }
+        d.s = r.s; d.m = r.m; d.bad |= r.bad;
+    }
+    d.s = warp_sum_pos(d.s);
+    if (first) cluster_wait();                              // every CTA of the cluster has started
+    if (lane < C) {
+        const uint32_t to = at_rank(&S.sum[w.rank * nw + warp], lane);
+        st_remote(to, d.s); st_remote(to + 8, d.top_s); st_remote(to + 16, d.W); st_remote(to + 24, d.A); st_remote(to + 32, d.B);
+        st_remote(to + 40, __float_as_int(d.m)); st_remote(to + 44, __float_as_int(d.top_m)); st_remote(to + 48, d.bad);
+    }
+    cluster_sync();
+    if (warp == 0) {
+        d = warp_merge<FAR>(S.sum, C * nw, c, inv_tau);
+        const DistillNumbers o = numbers<FAR>(a, w, d);
+        if (lane == 0) {
+            DistillGrad g;
+            const double G = (a.grad_loss ? (double)a.grad_loss[w.b] : 1.0) * inv_tau, Gq = G / o.total;
+            g.q = Gq * (o.P + o.r); g.w = G * o.k; g.M = o.M; g.nothing = o.nothing; g.far = o.far;
+            g.other = o.tail > 0.0 ? (float)(Gq * (o.P + o.r - (o.r > 0.0 ? o.r * o.total / o.tail : 0.0))) : 0.f;
+            S.grad = g;
+        }
+    }
+    __syncthreads();
+    const DistillGrad g = S.grad;                           // (the same in every CTA)
+    if (g.far) return true;
+    if (a.grad) gradient<DT, RES, FAR>(a, w, g);
+    if (warp == 0 && w.rank == 0) {
+        d = warp_merge<FAR>(S.sum, C * nw, c, inv_tau);
+        const DistillNumbers o = numbers<FAR>(a, w, d);
+        if (lane == 0) {
+            a.loss[w.b] = o.nothing ? 0.f : (float)kl(a, d, o);
+            if (a.row_status) a.row_status[w.b] = o.st;
+        }
+    }
+    return false;
+}
+template <int DT, bool RES> __device__ __noinline__ void distill_far(const DistillArgs& a, DistillShared& S, const DistillRow& w) {
+    cluster_sync();                                         // (every CTA has read the sums that are written again now)
+    distill_rest<DT, RES, true>(a, S, w, false);
+}
+
 }  // namespace
 
 template <int DT, bool RES>
-__global__ void __launch_bounds__(256, 2) k_distill(const __grid_constant__ DistillArgs a) {
+__global__ void __launch_bounds__(256, 3) k_distill(const __grid_constant__ DistillArgs a) {
     constexpr int VEC = Elem<DT>::VEC;
     extern __shared__ __align__(128) unsigned char smem[];
     __shared__ DistillShared S;
@@ -136,10 +305,12 @@ __global__ void __launch_bounds__(256, 2) k_distill(const __grid_constant__ Dist
     if (RES && wb > wa && !rows_wait(&S.bar[warp], 0)) bad |= 2;
     if (a.expire) bad |= 2;
     DSum d = no_dsum();
+    int mine = 0;
     const int t0 = (v0 + wa) * VEC, t1 = min((v0 + wb) * VEC, R.V);      // the warp's tokens
     for (int i = lane; i < T; i += 32) {
         const int id = ids[i];
         if (id < t0 || id >= t1) continue;
+        mine = 1;
         const int at = id - v0 * VEC;
         if (atomicOr(&bits[at >> 5], 1u << (at & 31)) >> (at & 31) & 1) { bad |= 4; continue; }      // (given twice)
         const float z = load_one<DT>(reinterpret_cast<const char*>(sl.p), at), t = teacher(i);
@@ -153,106 +324,29 @@ __global__ void __launch_bounds__(256, 2) k_distill(const __grid_constant__ Dist
         }
     }
     bad = __reduce_or_sync(0xffffffffu, bad);
+    mine = __any_sync(0xffffffffu, mine);
     d.top_m = ord2f(redux_max(f2ord(d.top_m)));
-    if (!(bad & 5))
+    if (mine && !(bad & 5)) {
         for (int i = lane; i < T; i += 32) {
             const int id = ids[i];
             if (id < t0 || id >= t1) continue;
             const float z = ez[i];
-            const double w = ew[i], x = ((double)z - (double)d.top_m) * inv_tau;
-            if (z > -INFINITY) d.top_s += q_exp2(((double)z - (double)d.top_m) * c.d, g_pow2_64);
+            const double w = ew[i], below = (double)d.top_m - (double)z;
+            if (z > -INFINITY) d.top_s += q_exp2(-below * c.d, g_pow2_64);
             if (w > 0.0) {
                 d.W += w;
-                d.A += w * (((double)teacher(i) - (double)tmax) * inv_tau);
-                d.B += z > -INFINITY ? w * x : -INFINITY;
+                d.A += w * (((double)tmax - (double)teacher(i)) * inv_tau);
+                if (z > -INFINITY) d.B += w * (below * inv_tau); else bad |= 8;
             }
         }
+        d.top_s = warp_sum(d.top_s); d.W = warp_sum(d.W); d.A = warp_sum(d.A); d.B = warp_sum(d.B);
+        bad = __reduce_or_sync(0xffffffffu, bad);
+    }
     __syncwarp();
-    // ---- pass 1: the sum of what is left
+    const DistillRow row{sl, reinterpret_cast<uint32_t*>(bits), ez, ew, ids, c, inv_tau, tau, lse, d, bad, valid, rank, b, wa, wb, v0, t0, t1, tmax};
     if (RES) {
-        const RSum r = warp_row_sum<DT, true, true>(sl, wa, wb, c);
-        d.s = r.s; d.m = r.m; bad |= r.bad;
-    } else {
-        RSum r = no_sum();
-        for (int v = wa; v < wb; v += 32) {
-            const int vi = v + lane;
-            const uint4 x = vi < wb ? without_entries<DT>(row_vec<DT, false>(sl, vi), entry_bits<DT>(bits, vi)) : neg_inf_vec<DT>();
-            const float wm = ord2f(redux_max(f2ord(max_nan(vec_max<DT>(x), -INFINITY))));
-            if (!(wm < INFINITY)) { r.bad = 1; continue; }
-            if (wm == -INFINITY) continue;
-            if (!(wm <= r.m + c.slack)) { r.s *= ref_factor(r.m, wm, c.d); r.m = wm; }
-            float e[VEC];
-            row_exp<DT, true>(x, r.m, c, e);
-            r.s += (double)sum_fixed<VEC>(e);
-        }
-        d.s = r.s; d.m = r.m; bad |= r.bad;
-    }
-    d.bad = bad;
-    d = warp_merge(d, c.d, inv_tau);
-    if (lane == 0) S.warp[warp] = d;
-    cluster_wait();                                         // every CTA of the cluster has started
-    __syncthreads();
-    if (warp == 0) {
-        d = warp_merge(lane < nw ? S.warp[lane] : no_dsum(), c.d, inv_tau);
-        if (lane < C) {
-            const uint32_t to = at_rank(&S.cta[rank], lane);
-            st_remote(to, d.s); st_remote(to + 8, d.top_s); st_remote(to + 16, d.W); st_remote(to + 24, d.A); st_remote(to + 32, d.B);
-            st_remote(to + 40, __float_as_int(d.m)); st_remote(to + 44, __float_as_int(d.top_m)); st_remote(to + 48, d.bad);
-        }
-    }
-    cluster_sync();
-    d = warp_merge(lane < C ? S.cta[lane] : no_dsum(), c.d, inv_tau);
-    const float M = fmaxf(d.m, d.top_m);
-    const double tail = d.s * ref_factor(d.m, M, c.d), top = d.top_s * ref_factor(d.top_m, M, c.d), total = tail + top;
-    int st = 0;
-    if (d.bad & 2) st = ST_WAIT;
-    else if (!tau_ok(tau)) st = ST_BAD_TEMP;
-    else if (d.bad & 4) st = ST_BAD_TOKEN;
-    else if (valid) st = (d.bad & 1) || !(total == total) ? ST_NONFINITE : M == -INFINITY || (!a.lse && !(d.W > 0.0)) ? ST_EMPTY : 0;
-    const bool nothing = st != 0 || !valid;                 // (the same in every CTA)
-    // ---- the loss
-    const double logk = a.lse ? (double)tmax * inv_tau - (double)lse : -log(d.W), k = a.lse ? (d.W > 0.0 ? exp(logk) : 0.0) : 1.0 / d.W;
-    const double P = a.lse ? k * d.W : 1.0, r = a.lse ? fmax(1.0 - P, 0.0) : 0.0;
-    if (rank == 0 && tid == 0) {
-        double loss = 0.0;
-        if (!nothing) {
-            const double logS = log(total);
-            if (d.W > 0.0) loss = k * d.A + P * logk - (k * (d.B + moved(d.W, d.top_m, M, inv_tau)) - P * logS);
-            if (r > 0.0) loss += r * (log(r) - log(tail) + logS);
-        }
-        a.loss[b] = (float)loss;
-        if (a.row_status) a.row_status[b] = st;
-    }
-    if (!a.grad) return;
-    // ---- the gradient
-    unsigned char* const grow = a.grad + (int64_t)b * a.g_row_bytes;
-    const double G = nothing ? 0.0 : (a.grad_loss ? (double)a.grad_loss[b] : 1.0) * inv_tau, Gq = nothing ? 0.0 : G / total;
-    const float other = nothing || !(tail > 0.0) ? 0.f : (float)(Gq * (P + r - (r > 0.0 ? r * total / tail : 0.0)));
-    const float mref = nothing ? 0.f : M;
-    for (int v = wa + lane; v < wb; v += 32) {
-        float e[VEC];
-        if (nothing) {
-#pragma unroll
-            for (int i = 0; i < VEC; ++i) e[i] = 0.f;
-        } else {
-            uint4 x = row_vec<DT, RES>(sl, v);
-            if (!RES) x = without_entries<DT>(x, entry_bits<DT>(bits, v));
-            row_exp<DT, DT == 0>(x, mref, c, e);
-#pragma unroll
-            for (int i = 0; i < VEC; ++i) e[i] *= other;
-        }
-        store_vec<DT>(grow, v0 + v, R.V, e);
-    }
-    if (nothing) return;
-    __syncwarp();                                           // (the warp's entries, behind the vectors that hold them)
-    for (int i = lane; i < T; i += 32) {
-        const int id = ids[i];
-        if (id < t0 || id >= t1) continue;
-        const double q = ez[i] > -INFINITY ? q_exp2(((double)ez[i] - (double)M) * c.d, g_pow2_64) : 0.0;
-        const float x = (float)(Gq * (P + r) * q - G * k * ew[i]);
-        if (DT == 0) reinterpret_cast<float*>(grow)[id] = x;
-        else reinterpret_cast<unsigned short*>(grow)[id] = (unsigned short)(pack_bf16x2(x, 0.f) & 0xffffu);
-    }
+        if (distill_rest<DT, RES, false>(a, S, row, true)) distill_far<DT, RES>(a, S, row);
+    } else distill_rest<DT, RES, true>(a, S, row, true);
 }
 
 cudaError_t distill(const RowArgs& r, const int32_t* ids, const void* top, int top_dt, int T, const float* lse, const float* grad_loss, float* loss,

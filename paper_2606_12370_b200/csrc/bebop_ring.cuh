@@ -1,0 +1,253 @@
+// Rows that go through a CTA several times: what the kernels that take them so share.
+//
+// A unit (a row, a row pair) belongs to one CTA, or to a cluster of them where there are fewer units than SMs.  A warp owns a run of the unit's vectors and goes
+// through it once for every pass, in chunks of kRingChunk vectors of each row: the first time from DRAM, then out of L2.  The chunks arrive in the warp's own ring
+// in shared memory by bulk copies that its first lane asks for, one ring's length ahead, over the ends of passes and units; so what a pass has to wait for
+// is the meeting of the warps between two passes, a fraction of a microsecond against the tens that a pass over a long row takes.
+#pragma once
+#include "bebop_rows.cuh"
+
+namespace bebop {
+
+namespace {
+
+constexpr int kRingWarps = 16, kRingVecs = 6, kRingChunk = 32 * kRingVecs;      // warps of a CTA, at most; vectors per lane and row of a chunk; vectors of a chunk
+
+template <int N> struct Count { static constexpr int value = N; };
+
+__device__ __noinline__ bool ring_wait_long(uint32_t bar, uint32_t parity) {
+    for (uint32_t i = 0; i < kRowsSpin; ++i) { if (mbar_try(bar, parity)) return true; __nanosleep(32); }
+    return false;
+}
+
+// ROWS rows side by side; two slots of a chunk of each (one where a run is a single chunk).
+template <int DT, int ROWS> struct Ring {
+    static constexpr int VEC = Elem<DT>::VEC, PART = kRingChunk * 16, SLOT = ROWS * PART, BYTES = 2 * SLOT;      // bytes of a chunk of a row, of a slot, of a warp's ring
+    const unsigned char* buf;                 // the lane's place in it
+    uint32_t smem, bar;                       // the ring and its two barriers
+    const unsigned char* at[ROWS];            // the warp's runs of the unit that is being asked for
+    int bytes, off;                           // of a run; where the next chunk to ask for begins
+    uint32_t two, ask_slot, take_slot, phase;
+    bool edge, failed;                        // the row ends inside the run's last vector
+
+    __device__ __forceinline__ void init(unsigned char* b, unsigned long long* s, int len, int left0) {
+        buf = b + (threadIdx.x & 31) * 16; smem = smem_u32(b); bar = smem_u32(s);
+        bytes = len * 16; off = 0; two = len > kRingChunk; ask_slot = take_slot = phase = 0; failed = false;
+        edge = left0 < len * VEC;
+        if ((threadIdx.x & 31) == 0) {
+            mbar_init(&s[0], 1); mbar_init(&s[1], 1);
+            asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        }
+        __syncwarp();
+    }
+    // asks for the next chunk of the unit at `at`
+    __device__ __forceinline__ void ask() {
+        const int n = min(PART, bytes - off);
+        if ((threadIdx.x & 31) == 0) {
+            const uint32_t b = bar + 8 * ask_slot, to = smem + ask_slot * SLOT;
+            asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" :: "r"(b), "r"(ROWS * n) : "memory");
+#pragma unroll
+            for (int r = 0; r < ROWS; ++r)
+                asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" :: "r"(to + r * PART), "l"(at[r] + off), "r"(n), "r"(b) : "memory");
+        }
+        ask_slot ^= two;
+        off = off + PART >= bytes ? 0 : off + PART;
+    }
+    __device__ __forceinline__ void first() { if (bytes > 0) ask(); if (two) ask(); }
+    // One pass, by whole warps: f(the lane's first vector of a chunk, in shared memory; its bytes from the run's start; vectors of it a lane at least: kRingVecs, or 0 where it is
+    // the run's last and may end early).  `next`: where the next unit's run lies, if this is the unit's last pass (and there is one), else null.
+    template <typename F> __device__ __forceinline__ void chunks_of(bool last, const unsigned char* const* next, F&& f) {
+#pragma unroll 1
+        for (int rem = bytes; rem > 0; rem -= PART) {
+            const uint32_t b = bar + 8 * take_slot;
+            if (!mbar_try(b, phase) && !ring_wait_long(b, phase)) failed = true;
+            f(buf + take_slot * SLOT, bytes - rem, rem > PART || (rem == PART && !edge));
+            phase ^= take_slot | (two ^ 1);
+            take_slot ^= two;
+            __syncwarp();
+            // the slot is free: the chunk one ring's length ahead, of this unit or, behind its last pass, of the next
+            if (!last || rem > (two ? 2 * PART : PART)) ask();
+            else if (next) {
+                if (off == 0)
+#pragma unroll
+                    for (int r = 0; r < ROWS; ++r) at[r] = next[r];
+                ask();
+            }
+        }
+    }
+    // vector j of a lane's chunk; beyond the run (`rem` bytes from the chunk's start on) or the vocabulary (`left` tokens) masked
+    static __device__ __forceinline__ uint4 edge_vec(const unsigned char* b, int r, int j, int rem, int left) {
+        const int vi = j * 32 + (threadIdx.x & 31), l = left - vi * VEC;
+        uint4 x = neg_inf_vec<DT>();
+        if (vi * 16 < rem) x = *reinterpret_cast<const uint4*>(b + r * PART + j * 512);
+        if (l < VEC) mask_tail<DT>(x, max(l, 0));
+        return x;
+    }
+    static __device__ __forceinline__ uint4 whole_vec(const unsigned char* b, int r, int j) { return *reinterpret_cast<const uint4*>(b + r * PART + j * 512); }
+    // ... vector by vector: f(its bytes from the run's start, the vectors of the rows, whether it lies inside the run and the vocabulary), and g(the lane's place in a chunk, its bytes from the run's start) behind every chunk.
+    // `left0`: tokens of the vocabulary from the run's first on.
+    template <typename F, typename G> __device__ __forceinline__ void pass(int left0, bool last, const unsigned char* const* next, F&& f, G&& g) {
+        const int lane = threadIdx.x & 31;
+        chunks_of(last, next, [&](const unsigned char* b, int from, bool whole) {
+            if (whole) {
+#pragma unroll
+                for (int j = 0; j < kRingVecs; ++j) {
+                    uint4 x[ROWS];
+#pragma unroll
+                    for (int r = 0; r < ROWS; ++r) x[r] = whole_vec(b, r, j);
+                    f(from + (j * 32 + lane) * 16, x, Count<1>());
+                }
+            } else {
+                const int rem = bytes - from, left = left0 - (from >> 4) * VEC;
+#pragma unroll 1
+                for (int j = 0; j < kRingVecs && j * 512 < rem; ++j) {
+                    uint4 x[ROWS];
+#pragma unroll
+                    for (int r = 0; r < ROWS; ++r) x[r] = edge_vec(b, r, j, rem, left);
+                    f(from + (j * 32 + lane) * 16, x, Count<0>());
+                }
+            }
+            g(b, from);
+        });
+    }
+    // ... the same for what is seldom called: a small loop (its instructions come from memory first, by the 128 bytes; six vectors' worth of them cost 25 us, this 2)
+    template <typename F, typename G> __device__ __forceinline__ void pass_small(int left0, bool last, const unsigned char* const* next, F&& f, G&& g) {
+        const int lane = threadIdx.x & 31;
+        chunks_of(last, next, [&](const unsigned char* b, int from, bool) {
+            const int rem = bytes - from, left = left0 - (from >> 4) * VEC;
+#pragma unroll 1
+            for (int j = 0; j < kRingVecs && j * 512 < rem; ++j) {
+                uint4 x[ROWS];
+#pragma unroll
+                for (int r = 0; r < ROWS; ++r) x[r] = edge_vec(b, r, j, rem, left);
+                f(from + (j * 32 + lane) * 16, x, Count<0>());
+            }
+            g(b, from);
+        });
+    }
+    // A pass for the rows' softmax sums: around the exponent of the warp's largest logit so far, a chunk's (at the end of a run a vector's) tokens in fp32, those in double.
+    struct Sum { double s, s2; int e; float ef, top; bool bad; };      // (s2: of the squares)
+    template <bool LOW, bool SQUARES> __device__ __forceinline__ void sums(int left0, bool last, const unsigned char* const* next, const RScale& c, Sum* o) {
+#pragma unroll
+        for (int r = 0; r < ROWS; ++r) { o[r].s = o[r].s2 = 0.0; o[r].e = E_EMPTY; o[r].ef = 0.f; o[r].top = -INFINITY; o[r].bad = false; }
+        const auto into = [&](Sum& a, const uint4* x, auto count) {
+            constexpr int N = decltype(count)::value;
+            const float m = N > 1 ? vecs_max<DT, N>(x) : max_nan(vec_max<DT>(x[0]), -INFINITY);
+            if (!__all_sync(0xffffffffu, m <= a.top)) {       // (also a NaN; hardly ever after the first chunks)
+                const QExp E = chunk_exponent(m, c.c);
+                if (E.e == E_BAD) a.bad = true;
+                else if (E.e > a.e) {
+                    const double f = a.e == E_EMPTY ? 0.0 : pow2d(max(a.e - E.e, -500));
+                    a.s *= f; a.s2 *= f * f;
+                    a.e = E.e; a.ef = E.ef;
+                    a.top = (E.ef - 0.0625f) / c.c;           // (a margin beyond every rounding: what is not above it has x c <= e)
+                }
+            }
+            float2 s0 = make_float2(0.f, 0.f), s1 = s0, s2 = s0;
+#pragma unroll
+            for (int j = 0; j < N; ++j) {
+                float e[VEC];
+                row_exp<DT, LOW, false>(x[j], a.ef, c, e);
+#pragma unroll
+                for (int q = 0; q < VEC; q += 4) { s0 = __fadd2_rn(s0, make_float2(e[q], e[q + 1])); s1 = __fadd2_rn(s1, make_float2(e[q + 2], e[q + 3])); }
+                if (SQUARES) {
+#pragma unroll
+                    for (int q = 0; q < VEC; q += 2) s2 = __ffma2_rn(make_float2(e[q], e[q + 1]), make_float2(e[q], e[q + 1]), s2);
+                }
+            }
+            a.s += (double)((s0.x + s0.y) + (s1.x + s1.y));
+            if (SQUARES) a.s2 += (double)(s2.x + s2.y);
+        };
+        chunks_of(last, next, [&](const unsigned char* b, int from, bool whole) {
+            if (whole) {
+#pragma unroll
+                for (int r = 0; r < ROWS; ++r) {
+                    uint4 x[kRingVecs];
+#pragma unroll
+                    for (int j = 0; j < kRingVecs; ++j) x[j] = whole_vec(b, r, j);
+                    into(o[r], x, Count<kRingVecs>());
+                }
+            } else {
+                const int rem = bytes - from, left = left0 - (from >> 4) * VEC;
+#pragma unroll 1
+                for (int j = 0; j < kRingVecs && j * 512 < rem; ++j)
+#pragma unroll
+                    for (int r = 0; r < ROWS; ++r) { const uint4 x = edge_vec(b, r, j, rem, left); into(o[r], &x, Count<1>()); }
+            }
+        });
+    }
+};
+
+// The warps' records, merged by a warp over its lanes (merge(records, n)), over the CTA and, through distributed shared memory, the cluster: the same in every
+// warp.  `warps` and `ctas` must not be in use any more; a second meeting takes others.
+template <typename R, typename F> __device__ __forceinline__ R meet(R* warps, R* ctas, const R& mine, int C, int rank, F&& merge) {
+    static_assert(sizeof(R) % 16 == 0, "records are sent in words");
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, nw = blockDim.x >> 5;
+    if (lane == 0) warps[warp] = mine;
+    __syncthreads();
+    if (C == 1) return merge(warps, nw);
+    if (warp == 0) {
+        const R r = merge(warps, nw);
+        if (lane < C) {
+            const uint32_t d = at_rank(&ctas[rank], lane);
+            const int* const v = reinterpret_cast<const int*>(&r);
+#pragma unroll
+            for (int i = 0; i < (int)sizeof(R) / 4; ++i) st_remote(d + 4 * i, v[i]);
+        }
+    }
+    cluster_sync();
+    return merge(ctas, C);
+}
+
+struct RingShape { int C, sv, threads, clusters, bytes; };      // CTAs per unit, vectors per slice, threads, clusters of the grid, dynamic shared memory
+
+// How many CTAs (clusters) of a kernel the device holds at a time (asked once per device and shape; 0: not known).
+template <auto kernel> int ring_resident(int C, int threads, int bytes) {
+    static int cached[64][kRowsMaxCluster + 1][kRingWarps + 1] = {{{0}}};
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) { cudaGetLastError(); return 0; }
+    int& n = cached[dev][C][threads / 32];
+    if (n) return n > 0 ? n : 0;
+    int got = 0;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = C; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)C); cfg.blockDim = dim3(threads); cfg.dynamicSmemBytes = bytes; cfg.attrs = attr; cfg.numAttrs = 1;
+    if (rows_ready<kernel>() != cudaSuccess || cudaOccupancyMaxActiveClusters(&got, kernel, &cfg) != cudaSuccess) { cudaGetLastError(); got = 0; }
+    n = got > 0 ? got : -1;
+    return got > 0 ? got : 0;
+}
+
+// The cut of a call of `units` units of `held` rows of nvec vectors; `extra`: shared memory of a CTA beside the rings, for a slice of sv vectors.
+template <auto kernel, typename E> cudaError_t ring_shape(int units, int held, int nvec, int ring_bytes, E&& extra, RingShape& s) {
+    const cudaError_t e = rows_ready<kernel>();
+    if (e != cudaSuccess) return e;
+    const int sms = rows_sms() > 0 ? rows_sms() : 148;
+    s.C = 1;
+    while (s.C < kRowsMaxCluster && (long long)units * (s.C + 1) <= sms && nvec > s.C * 1024) ++s.C;
+    // (the units under way at a time stay in L2 between their passes)
+    while (s.C < kRowsMaxCluster && (double)sms / s.C * nvec * 16.0 * held > 96e6) ++s.C;
+    s.sv = (nvec + s.C - 1) / s.C;
+    int warps = (s.sv + kRingChunk - 1) / kRingChunk;
+    warps = warps < 2 ? 2 : warps > kRingWarps ? kRingWarps : warps;
+    for (;; --warps) {
+        s.threads = 32 * warps;
+        s.bytes = warps * ring_bytes + extra(s.sv);
+        if (s.bytes <= kRowsSmem || warps == 1) break;
+    }
+    if (s.bytes > kRowsSmem) return cudaErrorInvalidConfiguration;
+    s.clusters = ring_resident<kernel>(s.C, s.threads, s.bytes);
+    if (s.clusters <= 0) s.clusters = 1;
+    if (s.clusters > units) s.clusters = units;
+    return cudaSuccess;
+}
+template <auto kernel, typename A> cudaError_t ring_launch(const A& args, const RingShape& s, cudaStream_t stream) {
+    RowsShape r;
+    r.C = s.C; r.threads = s.threads; r.bytes = s.bytes; r.sv = s.sv; r.res = false;
+    return rows_launch<kernel>(args, s.clusters, r, stream);
+}
+
+}  // namespace
+
+}  // namespace bebop

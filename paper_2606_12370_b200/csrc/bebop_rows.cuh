@@ -1,11 +1,11 @@
 // What the kernels that take a row (a row pair) by a cluster of CTAs and need no other launch share: the slice of a row that a
-// CTA holds, its softmax sums around float references, the exchange of the CTAs' sums, the launch.
+// CTA holds, its softmax sums, the exchange of the CTAs' sums, the launch.
 //
-// A softmax sum here is (m, s) with s = sum 2^((x - m) c), c = log2(e) / tau as two floats.  The difference x - m comes first, so
-// rows of any finite size are evaluated as defined: a row of nothing but a mask of -1e9, or of the type's lowest value, gives
-// equal weights.  (The kernels with integer exponents save an addition per two logits by fma(x, c, -E) and need a bound on |x c|.)
-// m is a reference, not the maximum: a warp keeps its first chunk's and moves it only when a chunk lies 2^16 above it, so that its
-// running sum is hardly ever rescaled.
+// A softmax sum is (m, s) with s = sum 2^(x c - m), c = log2(e) / tau: m is a whole number near the largest x c, so that sums are merged by exact
+// powers of two, and fma(x, c, -m) carries one rounding of a small number.  m is a reference, not the maximum: a warp keeps its first
+// chunk's and moves it when a chunk lies above it.  Rows whose largest |x c| lies beyond 2^22 -- nothing but a mask of -1e9 or of the type's lowest
+// value, a temperature next to zero -- are FAR: they are evaluated once more with the difference in front, 2^((x - m) c), m a logit, which holds for
+// finite logits of any size and costs an addition per two logits more.
 #pragma once
 #include "bebop_chunk.cuh"
 
@@ -13,29 +13,40 @@ namespace bebop {
 
 namespace {
 
-constexpr int RV = 4;                         // vectors per lane of a chunk
+constexpr int RV = 4;                        // vectors per lane of a chunk
 constexpr int RCV = 32 * RV;                  // vectors per chunk
 constexpr int kRowsMaxCluster = 16;
-constexpr int kRowsMaxWarps = 16;
-constexpr int kRowsSmem = 232448 - 4096;      // dynamic shared memory of a CTA, at most (the rest: static tables)
-constexpr uint32_t kRowsSpin = 1u << 24;
-constexpr float kRowsSlack = 16.f;            // a sum's terms are at most 2^kRowsSlack
+constexpr int kRowsMaxWarps = 8, kRowsMaxParts = kRowsMaxWarps * kRowsMaxCluster;
+constexpr int kRowsSmem = 232448 - 12288;     // dynamic shared memory of a CTA, at most (the rest: static tables)
+constexpr uint32_t kRowsSpin = 1u << 22;
+constexpr float kRowsSlack = 16.f;            // FAR: a sum's terms are at most 2^kRowsSlack (else 1)
 
 // log2(e) / tau, finite whatever tau, so that 0 * c is 0: to double precision (d), as the nearest float (c), and as a sum of floats hi + lo with lo
 // above 0, so that a masked logit's -inf stays -inf in both products.
-struct RScale { double d; float c, hi, lo, slack; };      // slack: kRowsSlack in units of logits
+struct RScale { double d; float c, hi, lo; };
 __device__ __forceinline__ RScale rows_scale(float tau) {
     RScale r;
     r.d = fmin(1.4426950408889634 / (tau_ok(tau) ? (double)tau : 1.0), 3e38);
     r.c = (float)r.d;
     r.hi = __int_as_float(__float_as_int(__double2float_rd(r.d)) - 1);
     r.lo = fmaxf((float)(r.d - (double)r.hi), 1e-45f);
-    r.slack = (float)((double)kRowsSlack / r.d);
     return r;
 }
 
 struct __align__(16) RSum { double s; float m; int bad; };      // bad: bit 0 a NaN or +inf, bit 1 a wait that gave up
 __device__ __forceinline__ RSum no_sum() { RSum r; r.s = 0.0; r.m = -INFINITY; r.bad = 0; return r; }
+
+constexpr float kRowsFar = 4194304.f, kRowsClamp = 1073741824.f;      // 2^22; references end at 2^30, far inside FAR
+__device__ __forceinline__ bool sum_far(float m) { return fabsf(m) >= kRowsFar && m > -INFINITY; }
+// the reference that a chunk's maximum gives: a logit (FAR), or a whole number, the power of two above the largest term
+template <bool FAR> __device__ __forceinline__ float row_ref(float m, const RScale& c) { return FAR ? m : ceilf(fminf(fmaxf(m * c.hi, -kRowsClamp), kRowsClamp)); }
+// the factor that takes a sum around a to the reference b >= a; 0 where a is -inf
+template <bool FAR> __device__ __forceinline__ double ref_factor(float a, float b, const RScale& c) {
+    if (FAR) return a == -INFINITY ? 0.0 : exp2(fmax(((double)a - (double)b) * c.d, -1100.0));
+    return pow2d((int)fmaxf(a - b, -1100.f));                // (also: -inf, and -inf - -inf, which max takes as -1100)
+}
+// the exponent of logit x around reference m
+template <bool FAR> __device__ __forceinline__ double row_arg(float x, float m, const RScale& c) { return FAR ? ((double)x - (double)m) * c.d : fma((double)x, c.d, -(double)m); }
 
 // The slice of a row: vectors [v0, v0 + nv) of it, in shared memory (RES) or where the caller has them.
 struct Slice { const unsigned char* p; int v0, nv, V; };
@@ -53,69 +64,103 @@ __device__ __forceinline__ uint4 row_vec(const Slice& s, int vi) {
     return x;
 }
 
-// x - m of a vector's logits, and their scaled differences' exponentials, two at a time.  bf16 logits: the low part of c is
-// below what the result is rounded to.
-template <int DT, bool LOW>
+// The exponentials of a vector's logits around reference m, two at a time; LOW: with the low part of c.
+template <int DT, bool LOW, bool FAR>
 __device__ __forceinline__ void row_exp(const uint4& raw, float m, const RScale& c, float* e) {
     constexpr int VEC = Elem<DT>::VEC;
     float f[VEC];
     unpack<DT>(raw, f);
-    const float2 m2 = make_float2(-m, -m), c2 = LOW ? make_float2(c.hi, c.hi) : make_float2(c.c, c.c), l2 = make_float2(c.lo, c.lo);
+    const float ch = LOW ? c.hi : c.c;
+    const float2 m2 = make_float2(-m, -m), c2 = make_float2(ch, ch), l2 = make_float2(c.lo, c.lo);
 #pragma unroll
     for (int i = 0; i < VEC; i += 2) {
-        const float2 d = __fadd2_rn(make_float2(f[i], f[i + 1]), m2);
-        float2 t = __fmul2_rn(d, c2);
-        if (LOW) t = __ffma2_rn(d, l2, t);
+        float2 x = make_float2(f[i], f[i + 1]), t;
+        if (FAR) { x = __fadd2_rn(x, m2); t = __fmul2_rn(x, c2); } else t = __ffma2_rn(x, c2, m2);
+        if (LOW) t = __ffma2_rn(x, l2, t);
         e[i] = ex2f(t.x);
         e[i + 1] = ex2f(t.y);
     }
 }
 
-// (a - b) 2^.. of two references, exactly enough: 2^((a - b) c), 0 where a is -inf
-__device__ __forceinline__ double ref_factor(float a, float b, double c) { return a == -INFINITY ? 0.0 : exp2(fmax(((double)a - (double)b) * c, -1100.0)); }
+// Sum over a warp of numbers >= 0 (the same bits in every lane), exact to 2^-24 of each and 2^-40 of the largest: a power of two takes the largest into [1, 2),
+// then they are added as integers.  A tenth of the latency of five steps of double shuffles and additions.
+__device__ __forceinline__ double warp_sum_pos(double s) {
+    const float f = (float)s;
+    const int top = redux_max(__float_as_int(f)) & 0x7f800000;
+    const float scale = __int_as_float(0x7f000000 - max(top, 0x00800000));      // 2^(127 - e)
+    return warp_sum_fixed(f * scale) * __hiloint2double((1023 - 127 + (max(top, 0x00800000) >> 23)) << 20, 0);
+}
 
-// Sums of lanes [0, n) merged over a warp (the same bits in every lane).
-__device__ __forceinline__ RSum warp_merge(RSum r, double c) {
-    const int om = redux_max(f2ord(r.m));
+// Sums of the lanes merged over a warp (the same bits in every lane).
+template <bool FAR> __device__ __forceinline__ RSum warp_merge(RSum r, const RScale& c) {
     RSum o;
-    o.m = ord2f(om);
+    o.m = ord2f(redux_max(f2ord(r.m)));
     o.bad = __reduce_or_sync(0xffffffffu, r.bad);
-    o.s = warp_sum(r.s * ref_factor(r.m, o.m, c));
+    o.s = warp_sum_pos(r.s * ref_factor<FAR>(r.m, o.m, c));
     return o;
 }
 
-// A warp's sum over vectors [a, b) of a slice: the lanes' parts in double, not yet added over the warp (s differs by lane).
-template <int DT, bool RES, bool LOW>
-__device__ __forceinline__ RSum warp_row_sum(const Slice& sl, int a, int b, const RScale& c) {
+// A chunk of RV vectors a lane into a warp's running sum, whose s differs by lane.
+template <int DT, bool LOW, bool FAR>
+__device__ __forceinline__ void chunk_into(RSum& r, const uint4* x, const RScale& c) {
     constexpr int VEC = Elem<DT>::VEC;
+    const float wm = ord2f(redux_max(f2ord(vecs_max<DT, RV>(x))));
+    if (!(wm < INFINITY)) { r.bad = 1; return; }
+    if (wm == -INFINITY) return;
+    const float m = row_ref<FAR>(wm, c);
+    if (FAR ? !((m - r.m) * c.hi <= kRowsSlack) : m > r.m) {      // (also: the first chunk with a logit)
+        r.s *= ref_factor<FAR>(r.m, m, c);
+        r.m = m;
+    }
+    float2 s0 = make_float2(0.f, 0.f), s1 = s0;
+#pragma unroll
+    for (int j = 0; j < RV; ++j) {
+        float e[VEC];
+        row_exp<DT, LOW, FAR>(x[j], r.m, c, e);
+#pragma unroll
+        for (int q = 0; q < VEC; q += 4) { s0 = __fadd2_rn(s0, make_float2(e[q], e[q + 1])); s1 = __fadd2_rn(s1, make_float2(e[q + 2], e[q + 3])); }
+    }
+    r.s += (double)((s0.x + s0.y) + (s1.x + s1.y));
+}
+
+// A warp's sum over vectors [a, b) of a slice: the lanes' parts in double, not yet added over the warp.  The vectors before `full` lie inside the vocabulary.
+template <int DT, bool RES, bool LOW, bool FAR>
+__device__ __forceinline__ RSum warp_row_sum(const Slice& sl, int a, int b, const RScale& c) {
     const int lane = threadIdx.x & 31;
     RSum r = no_sum();
-    for (int v = a; v < b; v += RCV) {
+    int v = a;
+    const int full = min(b, sl.V / Elem<DT>::VEC - sl.v0);
+    for (; v + RCV <= full; v += RCV) {
+        uint4 x[RV];
+#pragma unroll
+        for (int j = 0; j < RV; ++j) {
+            const unsigned char* const p = sl.p + (size_t)(v + j * 32 + lane) * 16;
+            x[j] = RES ? *reinterpret_cast<const uint4*>(p) : ldg16_stream(p);
+        }
+        chunk_into<DT, LOW, FAR>(r, x, c);
+    }
+    for (; v < b; v += RCV) {
         uint4 x[RV];
 #pragma unroll
         for (int j = 0; j < RV; ++j) { const int vi = v + j * 32 + lane; x[j] = vi < b ? row_vec<DT, RES>(sl, vi) : neg_inf_vec<DT>(); }
-        const float wm = ord2f(redux_max(f2ord(vecs_max<DT, RV>(x))));
-        if (!(wm < INFINITY)) { r.bad = 1; continue; }
-        if (wm == -INFINITY) continue;
-        if (!(wm <= r.m + c.slack)) {                          // (also: the first chunk with a logit)
-            r.s *= ref_factor(r.m, wm, c.d);
-            r.m = wm;
-        }
-        float2 s0 = make_float2(0.f, 0.f);
-#pragma unroll
-        for (int j = 0; j < RV; ++j) {
-            float e[VEC];
-            row_exp<DT, LOW>(x[j], r.m, c, e);
-#pragma unroll
-            for (int q = 0; q < VEC; q += 2) s0 = __fadd2_rn(s0, make_float2(e[q], e[q + 1]));
-        }
-        r.s += (double)(s0.x + s0.y);
+        chunk_into<DT, LOW, FAR>(r, x, c);
     }
     return r;
 }
 
 // the warp's sum, added over its lanes
-__device__ __forceinline__ RSum warp_total(RSum r) { r.s = warp_sum(r.s); return r; }
+__device__ __forceinline__ RSum warp_total(RSum r) { r.s = warp_sum_pos(r.s); return r; }
+// n sums, wherever they come from, as a lane's share of them: the entries lane, lane + 32, ... around the largest reference
+template <bool FAR> __device__ __forceinline__ RSum lane_share(const RSum* s, int n, const RScale& c) {
+    RSum r = no_sum();
+    for (int i = threadIdx.x & 31; i < n; i += 32) {
+        const RSum x = s[i];
+        const float m = fmaxf(r.m, x.m);
+        r.s = r.s * ref_factor<FAR>(r.m, m, c) + x.s * ref_factor<FAR>(x.m, m, c);
+        r.m = m; r.bad |= x.bad;
+    }
+    return r;
+}
 
 __device__ __forceinline__ void send_sum(RSum* at, const RSum& r, int rank) {
     const uint32_t d = at_rank(at, rank);
@@ -124,26 +169,27 @@ __device__ __forceinline__ void send_sum(RSum* at, const RSum& r, int rank) {
 
 __device__ __forceinline__ int sum_status(const RSum& r) {
     if (r.bad & 2) return ST_WAIT;
-    if ((r.bad & 1) || !(r.s == r.s)) return ST_NONFINITE;
+    if (r.bad & 1) return ST_NONFINITE;
     return r.m == -INFINITY ? ST_EMPTY : 0;
 }
 
 __device__ __forceinline__ bool rows_wait(unsigned long long* b, uint32_t parity) {
     const uint32_t addr = smem_u32(b);
-    for (uint32_t i = 0; i < kRowsSpin; ++i) if (mbar_try(addr, parity)) return true;
+    for (uint32_t i = 0; i < kRowsSpin; ++i) { if (mbar_try(addr, parity)) return true; __nanosleep(32); }
     return false;
 }
 
-// gradient vector `vi` of a row (in its own type) from floats; a vector that ends beyond the vocabulary by its elements
+// gradient vector `vi` of a row (in its own type) from floats
+template <int DT> __device__ __forceinline__ void store_whole(unsigned char* row, int vi, const float* f) {
+    const uint4 x = pack<DT>(f);
+    asm volatile("st.global.cs.v4.u32 [%0], {%1,%2,%3,%4};" :: "l"(row + (size_t)vi * 16), "r"(x.x), "r"(x.y), "r"(x.z), "r"(x.w) : "memory");
+}
+// ... that may end beyond the vocabulary: by its elements
 template <int DT>
 __device__ __forceinline__ void store_vec(unsigned char* row, int vi, int V, const float* f) {
     constexpr int VEC = Elem<DT>::VEC;
     const int left = V - vi * VEC;
-    if (left >= VEC) {
-        const uint4 x = pack<DT>(f);
-        asm volatile("st.global.cs.v4.u32 [%0], {%1,%2,%3,%4};" :: "l"(row + (size_t)vi * 16), "r"(x.x), "r"(x.y), "r"(x.z), "r"(x.w) : "memory");
-        return;
-    }
+    if (left >= VEC) { store_whole<DT>(row, vi, f); return; }
 #pragma unroll
     for (int i = 0; i < VEC; ++i) if (i < left) {
         if (DT == 0) reinterpret_cast<float*>(row)[(size_t)vi * VEC + i] = f[i];
@@ -198,7 +244,7 @@ RowsShape rows_shape(int rows, int held, int nvec, bool stream, int extra = 0, i
     s.res = !stream && bytes(kRowsMaxCluster) <= kRowsSmem;
     s.C = kRowsMaxCluster;
     if (s.res) {
-        const int share = 72000;
+        constexpr int share = 72000;                         // (so that three CTAs share an SM)
         s.C = 1;
         while (s.C < kRowsMaxCluster && bytes(s.C) > share) ++s.C;
         while (s.C < kRowsMaxCluster && (long long)rows * (s.C + 1) <= sms && (long long)held * nvec > (long long)s.C * 2048) ++s.C;
@@ -206,7 +252,7 @@ RowsShape rows_shape(int rows, int held, int nvec, bool stream, int extra = 0, i
     s.sv = slice(s.C);
     s.bytes = s.res ? held * s.sv * 16 : 0;
     int warps = (int)(((long long)held * s.sv + RCV - 1) / RCV);
-    warps = warps < 4 ? 4 : warps > 8 ? 8 : warps;
+    warps = warps < 4 ? 4 : warps > kRowsMaxWarps ? kRowsMaxWarps : warps;
     s.threads = 32 * warps;
     return s;
 }

@@ -27,7 +27,7 @@ struct TonlyArgs {
 };
 
 struct TonlyShared {
-    RSum warp[kRowsMaxWarps], cta[2][kRowsMaxCluster];      // (by the parity of the row: a CTA may be one row ahead)
+    RSum sum[2][kRowsMaxParts];                             // the warps' sums of all CTAs, by rank and warp; by the parity of the row: a CTA may be one row ahead
     double wmass[kRowsMaxWarps], cmass[kRowsMaxCluster];
     unsigned long long bar[kRowsMaxWarps];
     double tab[64];
@@ -36,7 +36,7 @@ struct TonlyShared {
 }  // namespace
 
 template <int DT, bool RES>
-__global__ void __launch_bounds__(256, 2) k_target_only(const __grid_constant__ TonlyArgs a) {
+__global__ void __launch_bounds__(256, 3) k_target_only(const __grid_constant__ TonlyArgs a) {
     constexpr int VEC = Elem<DT>::VEC;
     extern __shared__ __align__(128) unsigned char smem[];
     __shared__ TonlyShared S;
@@ -65,6 +65,9 @@ __global__ void __launch_bounds__(256, 2) k_target_only(const __grid_constant__ 
     int n = 0, x = -1;                                      // the row at hand; its draft
     Slice sl{smem, v0, nv, R.V};
     RSum tot = no_sum();
+    bool far = false;
+    auto arg = [&](float z) { return far ? row_arg<true>(z, tot.m, c) : row_arg<false>(z, tot.m, c); };
+    auto merge = [&](const RSum* s) { return far ? warp_merge<true>(lane_share<true>(s, C * nw, c), c) : warp_merge<false>(lane_share<false>(s, C * nw, c), c); };
     for (; !st; ++n) {
         const unsigned char* const g = reinterpret_cast<const unsigned char*>(row_ptr(R, b, n)) + (int64_t)v0 * 16;
         int bad = a.expire ? 2 : 0;
@@ -80,20 +83,21 @@ __global__ void __launch_bounds__(256, 2) k_target_only(const __grid_constant__ 
         } else sl.p = g;
         x = n < L ? __shfl_sync(0xffffffffu, tk, n) : -1;
         const float zx = n < L ? load_one<DT>(row_ptr(R, b, n), x) : 0.f;
-        RSum r = warp_total(warp_row_sum<DT, RES, true>(sl, wa, wb, c));
-        r.bad |= bad;
-        if (lane == 0) S.warp[warp] = r;
-        if (n == 0) cluster_wait();                         // every CTA of the cluster has started
-        __syncthreads();
-        if (warp == 0) {
-            r = warp_merge(lane < nw ? S.warp[lane] : no_sum(), c.d);
-            if (lane < C) send_sum(&S.cta[n & 1][rank], r, lane);
+        far = !RES;
+        for (;;) {
+            RSum r = warp_total(far ? warp_row_sum<DT, RES, true, true>(sl, wa, wb, c) : warp_row_sum<DT, RES, true, false>(sl, wa, wb, c));
+            r.bad |= bad;
+            if (n == 0 && !(RES && far)) cluster_wait();    // every CTA of the cluster has started
+            if (lane < C) send_sum(&S.sum[n & 1][rank * nw + warp], r, lane);
+            cluster_sync();
+            tot = merge(S.sum[n & 1]);
+            if (far || tot.bad || !sum_far(tot.m)) break;
+            far = true;
+            cluster_sync();                                 // (every CTA has read the sums that are written again now)
         }
-        cluster_sync();
-        tot = warp_merge(lane < C ? S.cta[n & 1][lane] : no_sum(), c.d);
         st = sum_status(tot);
         if (st || n == L) break;
-        const double p = q_exp2(((double)zx - (double)tot.m) * c.d, S.tab) / tot.s;
+        const double p = fmin(q_exp2(arg(zx), S.tab) / tot.s, 1.0);
         if (lane == n) px = p;
         if (!((double)__shfl_sync(0xffffffffu, u, n) < p)) break;
     }
@@ -115,7 +119,7 @@ __global__ void __launch_bounds__(256, 2) k_target_only(const __grid_constant__ 
         double s = 0.0;
 #pragma unroll
         for (int i = 0; i < VEC; ++i) {
-            m[i] = (v0 + vi) * VEC + i == x ? 0.0 : q_exp2(((double)f[i] - (double)tot.m) * c.d, S.tab);
+            m[i] = (v0 + vi) * VEC + i == x ? 0.0 : q_exp2(arg(f[i]), S.tab);
             s += m[i];
         }
         return s;

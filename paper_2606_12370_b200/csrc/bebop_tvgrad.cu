@@ -1,4 +1,4 @@
-// bebop_tv_grad: the TV loss of row pairs with its gradient in the draft logits, one cluster of CTAs per row pair.
+// bebop_tv_grad: the TV loss of row pairs with its gradient in the draft logits.
 //
 //   p, q = softmax(target / tau), softmax(draft / tau);  tv = sum max(0, p - q) = 1/2 sum |p - q|;  S = sum q 1[q <= p]
 //   gradient of g tv in draft logit v:  -(g / tau) q_v (1[q_v <= p_v] - S)                              (Eq. tv_grad)
@@ -8,19 +8,17 @@
 // theta, by the fp32 exponentials in the two sums.  A row pair that has a logit difference within the bound of that error is
 // evaluated again with sums in double, so that every comparison is the one that 64 bits give.
 //
-//   pass 1  the rows' softmax sums; the CTAs exchange theirs
-//   pass 2  sum |p - q|, S, the smallest |z_p - z_q - theta|; in place of the two logits their q with the comparison as its sign
-//           (a vector of each row gives 32 bytes: eight floats for bf16, in place of the draft's alone for fp32); exchange
-//   again   where that smallest distance is below the bound: sums in double from memory, and pass 2 once more
+// A CTA (a cluster of them, where there are fewer row pairs than SMs or rows are long) takes a row pair three times: the first time from DRAM, then out of L2.
+//   pass 1  the rows' softmax sums
+//   pass 2  sum |p - q|, S, the smallest |z_p - z_q - theta|
+//   again   where that smallest distance is below the bound: sums in double, and pass 2 once more
 //   pass 3  the gradient
 #include "bebop_kernels.h"
-#include "bebop_rows.cuh"
+#include "bebop_ring.cuh"
 
 namespace bebop {
 
 namespace {
-
-struct TvMass { double absum, signed_q, q; };        // sum |e_p - rho e_q|, sum of the signed and of the plain e_q
 
 struct TvGradArgs {
     RowArgs r;
@@ -29,218 +27,422 @@ struct TvGradArgs {
     int32_t* row_status;
     unsigned char* grad;
     int64_t g_row_bytes;
-    RowsShape s;
-    int expire;               // test hook: the wait for the rows counts as run out
-};
-
-struct TvGradShared {
-    RSum warp[2][kRowsMaxWarps], cta[2][kRowsMaxCluster];
-    double mass[3][kRowsMaxWarps], cta_mass[3][kRowsMaxCluster];
-    double wsum[2][kRowsMaxWarps], cta_sum[2][kRowsMaxCluster];
-    int near[kRowsMaxWarps], cta_near[kRowsMaxCluster];
-    unsigned long long bar[kRowsMaxWarps];
-    double tab[64];
-    int failed;
+    RingShape s;
+    int expire;               // test hook: a wait counts as run out
 };
 
 // What passes 2 and 3 need of a row pair.
 struct PairRef {
     float mp, mq;             // references
-    float rho_hi, rho_lo;     // S_p / S_q
+    float rho;                // S_p / S_q
     float theta;              // q <= p where z_p - z_q >= theta
-    float near;               // distances below this are not certain
+    float near;               // distances below it are not certain
     double theta_d;           // theta
 };
 
-__device__ __forceinline__ PairRef pair_ref(const RSum& p, const RSum& q, const RScale& c, float tau) {
+struct __align__(16) TvSums { RSum p, q; double p2, q2; };      // (p2, q2: sums of squares)
+
+// How far theta may be off, in units of tau.  Sums in fp32: every term carries an error of the order of 2^-24 (ex2.approx's bound is 2^-22) and of either sign, so
+// that a sum is off by 2^-24 sqrt(sum p^2), and by what the exponents' roundings have in common.  kNearKappa times that and kNearFloor: on 36,864 row pairs (1,024
+// to 151,936 tokens, N(0, 1) to N(0, 6^2), three temperatures, both types) the largest error is 0.6 of it.
+constexpr float kNearKappa = 4.5f, kNearFloor = 6e-8f;
+__device__ __forceinline__ float near_fp32(const TvSums& t) {
+    return kNearFloor + kNearKappa * 5.9604644775390625e-08f * ((float)(sqrt(t.p2) / t.p.s) + (float)(sqrt(t.q2) / t.q.s));
+}
+constexpr float kNearDouble = 1e-12f;                         // sums in double: 2.4e-15
+
+// FAR: the references are logits.
+template <bool FAR> __device__ __forceinline__ PairRef pair_ref(const RSum& p, const RSum& q, float tau, float near) {
     PairRef o;
     o.mp = p.m; o.mq = q.m;
-    const double rho = p.s / q.s;
-    o.rho_hi = (float)rho; o.rho_lo = (float)(rho - (double)o.rho_hi);
-    const double off = log2(rho) / c.d;                          // (lse_p - lse_q) tau - (mp - mq)
-    o.theta_d = ((double)p.m - (double)q.m) + off;
+    const double rho = p.s / q.s, unit = (double)tau * 0.6931471805599453;      // a logit's power of two
+    o.rho = (float)rho;
+    o.theta_d = (FAR ? 0.0 : ((double)p.m - (double)q.m) * unit) + log2(rho) * unit;      // (lse_p - lse_q) tau (FAR: less the references)
     o.theta = (float)o.theta_d;
-    // the sums' relative error, taken as 2^-22 each (ex2.approx's bound for every term; the sums' own is a tenth of it), moves theta by tau
-    // times that; the float difference of the logits and theta are off by half a step of theta each.  Beyond a float's range: always in double.
-    o.near = fabs(o.theta_d) < 1e38 ? (float)(4.76837158203125e-07 / (c.d * 0.6931471805599453) + 2.384185791015625e-07 * fabs(o.theta_d)) : INFINITY;
+    // the float difference of the logits and theta are off by half a step of theta each
+    o.near = near * tau + (float)(2.384185791015625e-07 * fabs(o.theta_d));
     return o;
 }
 
-// One vector pair: signed q (its sign: whether q > p), and the sums.  `exact`: distances below `near` are decided in double.
-template <int DT>
-__device__ __forceinline__ void pair_vec(const uint4& xp, const uint4& xq, const PairRef& R, const RScale& c, bool exact, float* sq,
-                                         float& absum, float& ssum, float& qsum, float& nearest) {
+__device__ __forceinline__ float min3_abs(float a, float b, float c) {      // of the magnitudes (NaN counts for nothing)
+    float d; asm("min.abs.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c)); return d;
+}
+__device__ __forceinline__ float sign_of(float u) { return __uint_as_float(0x3f800000u | (__float_as_uint(u) & 0x80000000u)); }      // 1 or -1
+__device__ __forceinline__ float2 minus2(float2 a, float2 b) { return __ffma2_rn(b, make_float2(-1.f, -1.f), a); }
+
+// z_p - z_q - theta of two tokens (NaN: masked in both rows, q = 0).  EXACT: distances below `near` in double; FAR: all of them, and each logit less its row's
+// largest first, as their difference may have no room for theta.
+template <bool FAR> __device__ __forceinline__ float exact_above(float u, float p, float q, const PairRef& R) {
+    if ((!FAR && fabsf(u) > R.near) || (p == -INFINITY && q == -INFINITY)) return u;
+    const double d = FAR ? ((double)p - (double)R.mp) - ((double)q - (double)R.mq) - R.theta_d : (double)p - (double)q - R.theta_d;
+    return d >= 0.0 ? fmaxf((float)d, 0.f) : fminf((float)d, -1e-45f);
+}
+template <bool FAR, bool EXACT> __device__ __forceinline__ float2 above(float p0, float p1, float q0, float q1, const PairRef& R) {
+    float2 u = __fadd2_rn(minus2(make_float2(p0, p1), make_float2(q0, q1)), make_float2(-R.theta, -R.theta));
+    if (EXACT) { u.x = exact_above<FAR>(u.x, p0, q0, R); u.y = exact_above<FAR>(u.y, p1, q1, R); }
+    return u;
+}
+// Pass 2 of one vector pair: sum |p - q| S_p, the q that are not above p less the others, (EXACT) all q, the smallest distance.
+struct PairAcc { float2 ab, ss, qs; float nearest; };
+__device__ __forceinline__ PairAcc no_acc() { PairAcc A; A.ab = make_float2(0.f, 0.f); A.ss = A.qs = A.ab; A.nearest = INFINITY; return A; }
+template <int DT, bool FAR, bool EXACT>
+__device__ __forceinline__ void pair_vec(const uint4& xp, const uint4& xq, const PairRef& R, const RScale& c, PairAcc& A) {
     constexpr int VEC = Elem<DT>::VEC;
-    float fp[VEC], fq[VEC], ep[VEC], eq[VEC];
+    float ep[VEC], eq[VEC], fp[VEC], fq[VEC];
+    row_exp<DT, DT == 0, FAR>(xp, R.mp, c, ep);
+    row_exp<DT, DT == 0, FAR>(xq, R.mq, c, eq);
     unpack<DT>(xp, fp); unpack<DT>(xq, fq);
-    row_exp<DT, DT == 0>(xp, R.mp, c, ep);
-    row_exp<DT, DT == 0>(xq, R.mq, c, eq);
+    const float2 rh = make_float2(-R.rho, -R.rho);
 #pragma unroll
-    for (int i = 0; i < VEC; ++i) {
-        float u = (fp[i] - fq[i]) - R.theta;                        // (NaN: masked in both rows, q = 0)
-        if (exact && !(fabsf(u) > R.near)) u = (double)fp[i] - (double)fq[i] >= R.theta_d ? 1.f : -1.f;
-        nearest = fminf(nearest, fabsf(u));
-        const float r = fmaf(-R.rho_lo, eq[i], fmaf(-R.rho_hi, eq[i], ep[i]));
-        absum += fabsf(r);
-        sq[i] = u >= 0.f ? eq[i] : -eq[i];
-        ssum += sq[i];
-        qsum += eq[i];
+    for (int i = 0; i < VEC; i += 2) {
+        const float2 q = make_float2(eq[i], eq[i + 1]), u = above<FAR, EXACT>(fp[i], fp[i + 1], fq[i], fq[i + 1], R);
+        A.nearest = min3_abs(u.x, u.y, A.nearest);
+        const float2 r = __ffma2_rn(rh, q, make_float2(ep[i], ep[i + 1])), s = make_float2(sign_of(u.x), sign_of(u.y));
+        A.ab = __ffma2_rn(r, s, A.ab);                       // (r has u's sign, but for roundings of its own size)
+        A.ss = __ffma2_rn(q, s, A.ss);
+        if (EXACT) A.qs = __fadd2_rn(A.qs, q);
+    }
+}
+// Pass 3 of one vector pair: q times `below` where it is not above p, times `over` where it is.
+template <int DT, bool FAR, bool EXACT>
+__device__ __forceinline__ void grad_vec(const uint4& xp, const uint4& xq, const PairRef& R, const RScale& c, float below, float over, float* g) {
+    constexpr int VEC = Elem<DT>::VEC;
+    float eq[VEC], fp[VEC], fq[VEC];
+    row_exp<DT, DT == 0, FAR>(xq, R.mq, c, eq);
+    unpack<DT>(xp, fp); unpack<DT>(xq, fq);
+#pragma unroll
+    for (int i = 0; i < VEC; i += 2) {
+        const float2 u = above<FAR, EXACT>(fp[i], fp[i + 1], fq[i], fq[i + 1], R);
+        const float2 o = __fmul2_rn(make_float2(eq[i], eq[i + 1]), make_float2(u.x >= 0.f ? below : over, u.y >= 0.f ? below : over));
+        g[i] = o.x; g[i + 1] = o.y;
     }
 }
 
-template <int DT> __device__ __forceinline__ void grad_vec(const float* sq, float below, float above, float* g) {
+struct __align__(16) TvMass { double ab, ss, q; int near, pad; };
+struct __align__(16) TvTwo { double a, b; };
+struct __align__(16) TvFour { double a, b, a2, b2; };
+constexpr int kTvOpen = 192;
+struct TvOpen { float p, q, e, s; };                         // a token's logits, its exponential of the draft's, the sign it was given
+struct TvGradShared {
+    TvSums sum[kRingWarps], cta_sum[kRowsMaxCluster];
+    TvMass mass[4][kRingWarps], cta_mass[4][kRowsMaxCluster];        // (pass 2, and three times more)
+    TvTwo max[kRingWarps], cta_max[kRowsMaxCluster], exact[2][kRingWarps], cta_exact[2][kRowsMaxCluster];
+    TvFour finer[kRingWarps], cta_finer[kRowsMaxCluster];
+    unsigned long long bar[kRingWarps][2];
+    int opens;                                               // tokens whose comparison is open: how many, the first of them,
+    unsigned long long open_mass;                            // what they weigh (2^-44), the smallest and the largest difference of their logits (ordered)
+    long long open_least, open_most;
+    TvOpen open[kTvOpen];
+};
+
+__device__ __forceinline__ RSum merge_sum(RSum r, double r2, double& o2, const RScale& c) {      // (in double: theta hangs on it)
+    RSum o;
+    o.m = ord2f(redux_max(f2ord(r.m)));
+    o.bad = __reduce_or_sync(0xffffffffu, r.bad);
+    const double f = ref_factor<false>(r.m, o.m, c);
+    o.s = warp_sum(r.s * f);
+    o2 = warp_sum(r2 * (f * f));
+    return o;
+}
+__device__ __forceinline__ TvMass merge_mass(const TvMass* s, int n) {
+    const int lane = threadIdx.x & 31;
+    TvMass m = {0.0, 0.0, 0.0, 0, 0};
+    if (lane < n) m = s[lane];
+    m.ab = warp_sum(m.ab); m.ss = warp_sum(m.ss); m.q = warp_sum(m.q);
+    m.near = __any_sync(0xffffffffu, m.near);
+    return m;
+}
+
+struct NoHook { __device__ __forceinline__ void operator()(const unsigned char*, int) const {} };
+using TvRing0 = Ring<0, 2>;
+using TvRing1 = Ring<1, 2>;
+
+// 2^t of two numbers <= 1 in fp32 by the series of 2^f, |f| <= 1/2, to the seventh power (the next term is 5e-9 at most, 6e-10 in the mean): unlike ex2.approx's, its errors
+// are roundings without a mean that would stay in a sum of thousands.  Below -120: next to nothing.
+__device__ __forceinline__ float2 series_exp2(float2 x, const RScale& c, float least, int down) {
+    // x c = n + f first, f exactly but for 2^-26: the exponent loses nothing to the size of x c - m
+    const float2 magic = make_float2(12582912.f, 12582912.f), hi = make_float2(c.hi, c.hi), lo = make_float2(c.lo, c.lo);
+    x.x = fmaxf(x.x, least); x.y = fmaxf(x.y, least);
+    const float2 r = __ffma2_rn(x, hi, magic), f = __ffma2_rn(x, lo, __ffma2_rn(x, hi, minus2(magic, r)));
+    const auto k = [](float a) { return make_float2(a, a); };
+    float2 p = __ffma2_rn(f, k(1.5252734e-5f), k(1.5403530e-4f));      // ln2^7 / 7!, ln2^6 / 6!, ...
+    p = __ffma2_rn(f, p, k(1.3333558e-3f));
+    p = __ffma2_rn(f, p, k(9.6181291e-3f));
+    p = __ffma2_rn(f, p, k(5.5504109e-2f));
+    p = __ffma2_rn(f, p, k(2.4022651e-1f));
+    p = __ffma2_rn(f, p, k(6.9314718e-1f));
+    p = __ffma2_rn(f, p, k(1.f));
+    return make_float2(__int_as_float(__float_as_int(p.x) + ((__float_as_int(r.x) - down) << 23)), __int_as_float(__float_as_int(p.y) + ((__float_as_int(r.y) - down) << 23)));
+}
+// The sums of a row pair whose comparisons are open, more exactly: the terms from 2^-7 of the largest on in double, the others (most, and light) by the series above,
+// whose errors have no mean: of near_finer's bound, ten to forty times below near_fp32's, the largest error on the row pairs above is 0.47.  A fifth of tv_exact's time.
+constexpr float kTvHeavy = 0.0078125f;
+template <int DT> __device__ __noinline__ void tv_finer(Ring<DT, 2>& held, TvGradShared& S, int left0, const RScale& scale, int rank, int C, TvSums& tot) {
+    constexpr int VEC = Elem<DT>::VEC;
+    const int lane = threadIdx.x & 31;
+    Ring<DT, 2> ring = held;
+    const RScale c = scale;
+    const int down[2] = {(int)tot.p.m, (int)tot.q.m};
+    const float least[2] = {(tot.p.m - 120.f) / c.hi, (tot.q.m - 120.f) / c.hi};
+    const float m[2] = {tot.p.m, tot.q.m};
+    double d[2] = {0.0, 0.0};
+    float h2[2] = {0.f, 0.f};
+    ring.chunks_of(false, nullptr, [&](const unsigned char* at, int from, bool) {
+        const int rem = ring.bytes - from, left = left0 - (from >> 4) * VEC;
+#pragma unroll 1
+        for (int j = 0; j < kRingVecs && j * 512 < rem; ++j) {
+            unsigned heavy = 0;
 #pragma unroll
-    for (int i = 0; i < Elem<DT>::VEC; ++i) g[i] = __float_as_int(sq[i]) >= 0 ? sq[i] * below : sq[i] * above;
+            for (int w = 0; w < 2; ++w) {
+                float f[VEC];
+                unpack<DT>(Ring<DT, 2>::edge_vec(at, w, j, rem, left), f);
+                float2 s = make_float2(0.f, 0.f);
+#pragma unroll
+                for (int i = 0; i < VEC; i += 2) {
+                    float2 e = series_exp2(make_float2(f[i], f[i + 1]), c, least[w], down[w]);
+                    if (e.x >= kTvHeavy) { heavy |= 1u << (w * VEC + i); e.x = 0.f; }
+                    if (e.y >= kTvHeavy) { heavy |= 2u << (w * VEC + i); e.y = 0.f; }
+                    s = __fadd2_rn(s, e);
+                }
+                d[w] += (double)(s.x + s.y);
+            }
+#pragma unroll 1
+            for (; heavy; heavy &= heavy - 1) {
+                const int i = __ffs(heavy) - 1, w = i / VEC;
+                const unsigned char* const z = at + w * Ring<DT, 2>::PART + j * 512 + (i % VEC) * (16 / VEC);
+                const float f = DT == 0 ? *reinterpret_cast<const float*>(z) : __uint_as_float((unsigned)*reinterpret_cast<const unsigned short*>(z) << 16);
+                const double e = q_exp2(row_arg<false>(f, w ? m[1] : m[0], c), g_pow2_64);
+                const float e2 = (float)(e * e);
+                if (w) { d[1] += e; h2[1] += e2; } else { d[0] += e; h2[0] += e2; }
+            }
+        }
+    });
+    held = ring;
+    const TvFour s = meet(S.finer, S.cta_finer, TvFour{warp_sum(d[0]), warp_sum(d[1]), warp_sum((double)h2[0]), warp_sum((double)h2[1])}, C, rank, [&](const TvFour* s, int n) {
+        return TvFour{warp_sum(lane < n ? s[lane].a : 0.0), warp_sum(lane < n ? s[lane].b : 0.0), warp_sum(lane < n ? s[lane].a2 : 0.0), warp_sum(lane < n ? s[lane].b2 : 0.0)};
+    });
+    tot.p.s = s.a; tot.q.s = s.b;
+    tot.p2 = fmax(tot.p2 - s.a2, 1e-5 * tot.p2); tot.q2 = fmax(tot.q2 - s.b2, 1e-5 * tot.q2);      // (the sums' own errors: 1e-6)
+}
+__device__ __forceinline__ float near_finer(const TvSums& t) { return 6e-9f + 4.f * 5.9604644775390625e-08f * ((float)(sqrt(t.p2) / t.p.s) + (float)(sqrt(t.q2) / t.q.s)); }
+
+// ... and all of them in double.  FAR: around the rows' largest logits, which are found first.
+template <int DT, bool FAR> __device__ __noinline__ void tv_exact(Ring<DT, 2>& ring, TvGradShared& S, int left0, const RScale& c, int rank, int C, TvSums& tot) {
+    constexpr int VEC = Elem<DT>::VEC;
+    const int lane = threadIdx.x & 31;
+    if (FAR) {
+        float mp = -INFINITY, mq = -INFINITY;
+        ring.pass_small(left0, false, nullptr, [&](int, const uint4* x, auto) { mp = fmaxf(mp, vec_max<DT>(x[0])); mq = fmaxf(mq, vec_max<DT>(x[1])); }, NoHook());
+        mp = ord2f(redux_max(f2ord(mp))); mq = ord2f(redux_max(f2ord(mq)));
+        const TvTwo m = meet(S.max, S.cta_max, TvTwo{(double)mp, (double)mq}, C, rank, [&](const TvTwo* s, int n) {
+            const float a = lane < n ? (float)s[lane].a : -INFINITY, b = lane < n ? (float)s[lane].b : -INFINITY;
+            return TvTwo{(double)ord2f(redux_max(f2ord(a))), (double)ord2f(redux_max(f2ord(b)))};
+        });
+        tot.p.m = (float)m.a; tot.q.m = (float)m.b;
+    }
+    double d[2] = {0.0, 0.0};
+    ring.pass_small(left0, false, nullptr, [&](int, const uint4* x, auto) {
+#pragma unroll
+        for (int w = 0; w < 2; ++w) {
+            const float m = w ? tot.q.m : tot.p.m;
+            float f[VEC];
+            unpack<DT>(x[w], f);
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) d[w] += q_exp2(row_arg<FAR>(f[i], m, c), g_pow2_64);
+        }
+    }, NoHook());
+    constexpr int k = FAR ? 1 : 0;
+    const TvTwo s = meet(S.exact[k], S.cta_exact[k], TvTwo{warp_sum(d[0]), warp_sum(d[1])}, C, rank, [&](const TvTwo* s, int n) {
+        return TvTwo{warp_sum(lane < n ? s[lane].a : 0.0), warp_sum(lane < n ? s[lane].b : 0.0)};
+    });
+    tot.p.s = s.a; tot.q.s = s.b;
+}
+
+// order-preserving whole number of a double that is a number
+__device__ __forceinline__ long long dord(double x) { const long long b = __double_as_longlong(x); return b ^ ((b >> 63) & 0x7fffffffffffffffLL); }
+
+// The tokens of a chunk whose comparison is open.
+template <int DT> __device__ __noinline__ void tv_collect(TvGradShared& S, const unsigned char* b, int rem, int left, const PairRef& R, const RScale& c) {
+    constexpr int VEC = Elem<DT>::VEC;
+    for (int j = 0; j < kRingVecs && j * 512 < rem; ++j) {
+        const uint4 xp = Ring<DT, 2>::edge_vec(b, 0, j, rem, left), xq = Ring<DT, 2>::edge_vec(b, 1, j, rem, left);
+        float eq[VEC], fp[VEC], fq[VEC];
+        row_exp<DT, DT == 0, false>(xq, R.mq, c, eq);
+        unpack<DT>(xp, fp); unpack<DT>(xq, fq);
+#pragma unroll
+        for (int i = 0; i < VEC; i += 2) {
+            const float2 u = above<false, false>(fp[i], fp[i + 1], fq[i], fq[i + 1], R);
+#pragma unroll
+            for (int k = 0; k < 2; ++k)
+                if (fabsf(k ? u.y : u.x) <= R.near) {
+                    const int at = atomicAdd(&S.opens, 1);
+                    if (at < kTvOpen) S.open[at] = {fp[i + k], fq[i + k], eq[i + k], sign_of(k ? u.y : u.x)};
+                    const long long d = dord((double)fp[i + k] - (double)fq[i + k]);
+                    atomicMin(&S.open_least, d); atomicMax(&S.open_most, d);
+                    atomicAdd(&S.open_mass, (unsigned long long)((double)eq[i + k] * 0x1p44));
+                }
+        }
+    }
 }
 
 }  // namespace
 
-template <int DT, bool RES>
-__global__ void __launch_bounds__(256, 2) k_tv_grad(const __grid_constant__ TvGradArgs a) {
+template <int DT>
+__global__ void __launch_bounds__(32 * kRingWarps, 1) k_tv_grad(const __grid_constant__ TvGradArgs a) {
     constexpr int VEC = Elem<DT>::VEC;
     extern __shared__ __align__(128) unsigned char smem[];
     __shared__ TvGradShared S;
     const RowArgs& R = a.r;
     const int C = a.s.C, sv = a.s.sv;
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, nw = blockDim.x >> 5;
-    const int rank = (int)cluster_rank(), b = (int)(blockIdx.x / (unsigned)C);
-    cluster_arrive();                                       // (waited for before the first store into another CTA)
-    if (lane == 0) { mbar_init(&S.bar[warp], 1); asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory"); }
-    if (tid < 64) S.tab[tid] = g_pow2_64[tid];
-    if (tid == 0) S.failed = a.expire;
-    __syncthreads();
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, nw = blockDim.x >> 5;
+    const int rank = (int)cluster_rank(), clusters = a.s.clusters;
+    const int v0 = rank * sv, nv = max(min(sv, R.nvec - v0), 0), per = (nv + nw - 1) / nw, wa = min(warp * per, nv), len = min(per, nv - wa);
+    const int left0 = R.V - (v0 + wa) * VEC;                // tokens from the warp's first vector on
+    Ring<DT, 2> ring;
+    ring.init(smem + (size_t)warp * Ring<DT, 2>::BYTES, S.bar[warp], len, left0);
     // (programmatic dependent launch: nothing of the caller's memory is touched until the grid before this one is through)
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-    const float tau = tau_of(R, b);
-    const RScale c = rows_scale(tau);
-    const int v0 = rank * sv, nv = max(min(sv, R.nvec - v0), 0);
-    const unsigned char* const gp = reinterpret_cast<const unsigned char*>(row_ptr(R, b, 0)) + (int64_t)v0 * 16;
-    const unsigned char* const gq = reinterpret_cast<const unsigned char*>(row_ptr(R, b, R.K + 1)) + (int64_t)v0 * 16;
-    const Slice mp{gp, v0, nv, R.V}, mq{gq, v0, nv, R.V};   // in memory
-    const Slice sp{RES ? smem : gp, v0, nv, R.V}, sq{RES ? smem + (size_t)sv * 16 : gq, v0, nv, R.V};
-    const int per = ((nv + nw - 1) / nw + 7) & ~7, wa = min(warp * per, nv), wb = min(wa + per, nv);      // the warp's vectors
-    if (RES && lane == 0 && wb > wa) {
-        const uint32_t bytes = (uint32_t)(wb - wa) * 16u;
-        mbar_arrive_expect(&S.bar[warp], 2 * bytes);
-        bulk_load(smem_u32(smem + (size_t)wa * 16), gp + (size_t)wa * 16, bytes, &S.bar[warp]);
-        bulk_load(smem_u32(smem + (size_t)(sv + wa) * 16), gq + (size_t)wa * 16, bytes, &S.bar[warp]);
-    }
-    // ---- pass 1
-    if (RES && wb > wa && !rows_wait(&S.bar[warp], 0)) S.failed = 1;
-    for (int w = 0; w < 2; ++w) {
-        const RSum r = warp_total(warp_row_sum<DT, RES, true>(w ? sq : sp, wa, wb, c));
-        if (lane == 0) S.warp[w][warp] = r;
-    }
-    cluster_wait();                                         // every CTA of the cluster has started
-    __syncthreads();
-    if (warp < 2) {
-        RSum r = lane < nw ? S.warp[warp][lane] : no_sum();
-        r = warp_merge(r, c.d);
-        if (S.failed) r.bad |= 2;
-        if (lane < C) send_sum(&S.cta[warp][rank], r, lane);
-    }
-    cluster_sync();
-    const RSum tp = warp_merge(lane < C ? S.cta[0][lane] : no_sum(), c.d), tq = warp_merge(lane < C ? S.cta[1][lane] : no_sum(), c.d);
-    int st = sum_status(tp) | sum_status(tq);
-    if (st & ST_WAIT) st = ST_WAIT;
-    else if (!tau_ok(tau)) st = ST_BAD_TEMP;
-    const float g = a.grad_tv ? a.grad_tv[b] : 1.f;
-    unsigned char* const grow = a.grad + (int64_t)b * a.g_row_bytes;
-    if (st) {                                               // (the same in every CTA)
-        float z[VEC];
+    const auto run_at = [&](int unit, const unsigned char** at) {
+        at[0] = reinterpret_cast<const unsigned char*>(row_ptr(R, unit, 0)) + (int64_t)(v0 + wa) * 16;
+        at[1] = reinterpret_cast<const unsigned char*>(row_ptr(R, unit, R.K + 1)) + (int64_t)(v0 + wa) * 16;
+    };
+    int u = (int)(blockIdx.x / (unsigned)C);
+    run_at(u, ring.at);
+    ring.first();
+    if (C > 1) cluster_sync();                              // every CTA of the cluster has started
+#pragma unroll 1
+    for (; u < R.B; u += clusters) {
+        const float tau = tau_of(R, u), g = a.grad_tv ? a.grad_tv[u] : 1.f;
+        const RScale c = rows_scale(tau);
+        unsigned char* const grow = a.grad + (int64_t)u * a.g_row_bytes + (int64_t)(v0 + wa) * 16;      // the warp's run of the gradient
+        const bool first = rank == 0 && threadIdx.x == 0;
+        // ---- pass 1
+        typename Ring<DT, 2>::Sum rs[2];
+        ring.template sums<DT == 0, true>(left0, false, nullptr, c, rs);
+        TvSums tot;
+        tot.p.s = warp_sum(rs[0].s); tot.q.s = warp_sum(rs[1].s); tot.p2 = warp_sum(rs[0].s2); tot.q2 = warp_sum(rs[1].s2);
+        tot.p.m = rs[0].e == E_EMPTY ? -INFINITY : (float)rs[0].e; tot.q.m = rs[1].e == E_EMPTY ? -INFINITY : (float)rs[1].e;
+        tot.p.bad = (rs[0].bad || rs[1].bad ? 1 : 0) | (a.expire || ring.failed ? 2 : 0); tot.q.bad = 0;
+        if (threadIdx.x == 0) { S.opens = 0; S.open_mass = 0; S.open_least = LLONG_MAX; S.open_most = LLONG_MIN; }                    // (nobody looks at the last unit's any more: a meeting lies behind)
+        tot = meet(S.sum, S.cta_sum, tot, C, rank, [&](const TvSums* s, int n) {
+            TvSums o, x;
+            x.p = x.q = no_sum(); x.p2 = x.q2 = 0.0;
+            if (lane < n) x = s[lane];
+            o.p = merge_sum(x.p, x.p2, o.p2, c); o.q = merge_sum(x.q, x.q2, o.q2, c);
+            return o;
+        });
+        int st = sum_status(tot.p) | sum_status(tot.q);
+        if (st & ST_WAIT) st = ST_WAIT;
+        else if (!tau_ok(tau)) st = ST_BAD_TEMP;
+        const unsigned char* next_at[2] = {nullptr, nullptr};
+        const bool more = u + clusters < R.B;
+        if (more) run_at(u + clusters, next_at);
+        PairRef ref = pair_ref<false>(tot.p, tot.q, tau, near_fp32(tot));
+        double tv = 0.0, s_aux = 0.0, scale = 0.0;
+        const bool far = !st && (far_exponent((int)tot.p.m) || far_exponent((int)tot.q.m));
+        bool again = far, wide = false;
+        if (st) ring.pass_small(left0, false, nullptr, [](int, const uint4*, auto) {}, NoHook());       // (the same in every CTA)
+        else {
+            // ---- pass 2
+            PairAcc A = no_acc();
+            double s_ab = 0.0, s_ss = 0.0, s_qs = 0.0;
+            int n = 0, open = 0;
+            const auto spill = [&] {
+                s_ab += (double)(A.ab.x + A.ab.y); s_ss += (double)(A.ss.x + A.ss.y); s_qs += (double)(A.qs.x + A.qs.y);
+                A = no_acc();
+                n = 0;
+            };
+            const auto part = [&] {
+                TvMass m;
+                m.ab = warp_sum(s_ab); m.ss = warp_sum(s_ss); m.q = wide ? warp_sum(s_qs) : 0.0; m.pad = 0;
+                m.near = open;
+                return m;
+            };
+            ring.pass(left0, false, nullptr, [&](int, const uint4* x, auto) { pair_vec<DT, false, false>(x[0], x[1], ref, c, A); }, [&](const unsigned char* b, int from) {
+                if (__any_sync(0xffffffffu, A.nearest <= ref.near)) {
+                    tv_collect<DT>(S, b, ring.bytes - from, left0 - (from >> 4) * VEC, ref, c);
+                    open = 1;
+                    A.nearest = INFINITY;
+                }
+                if (++n == 4) spill();
+            });
+            spill();
+            TvMass mass = meet(S.mass[0], S.cta_mass[0], part(), C, rank, merge_mass);
+            // ---- and again where a comparison is not certain, or a row FAR: the sums in double, by which the comparisons that were open are decided ...
+            again = far || mass.near;
+            int wide_too = far;
+            if (again && !far) {
+                const float near = ref.near;
+                for (int level = 0; level < 2; ++level) {
+                    Ring<DT, 2> r2 = ring;                  // (by a copy, so that the ring itself stays in registers)
+                    TvSums exact = tot;
+                    if (level == 0) tv_finer<DT>(r2, S, left0, c, rank, C, exact); else tv_exact<DT, false>(r2, S, left0, c, rank, C, exact);
+                    ring = r2;
+                    ref = pair_ref<false>(exact.p, exact.q, tau, 0.f);
+                    ref.near = near;
+                    const double still = (double)(level == 0 ? near_finer(exact) : kNearDouble) * (double)tau;
+                    TvMass m = {0.0, 0.0, 0.0, 0, 0};
+                    const int opens = S.opens;
+                    long long moved = 0;                    // (whole numbers: the tokens' order in the list does not matter)
+                    // (more than the list holds: on a grid of bf16 logits all at one difference, and decided alike)
+                    const bool alike = opens > kTvOpen && S.open_least == S.open_most;
+                    m.near = opens > kTvOpen && !alike;
+                    for (int i = threadIdx.x; i < (alike ? 1 : min(opens, kTvOpen)); i += blockDim.x) {
+                        const TvOpen o = S.open[i];
+                        const double d = (double)o.p - (double)o.q - ref.theta_d;
+                        if (fabs(d) <= still) m.near = 1;
+                        const long long e = alike ? (long long)S.open_mass : (long long)((double)o.e * 0x1p44);
+                        if ((d >= 0.0) != (o.s > 0.f)) moved += d >= 0.0 ? e : -e;
+                    }
 #pragma unroll
-        for (int i = 0; i < VEC; ++i) z[i] = 0.f;
-        for (int v = tid; v < nv; v += blockDim.x) store_vec<DT>(grow, v0 + v, R.V, z);
-        if (rank == 0 && tid == 0) {
-            if (a.tv) a.tv[b] = 0.f;
-            if (a.s_aux) a.s_aux[b] = 0.f;
-            if (a.row_status) a.row_status[b] = st;
-        }
-        return;
-    }
-    PairRef ref = pair_ref(tp, tq, c, tau);
-    // ---- pass 2, and again where a comparison is not certain
-    bool again = false;
-    for (;;) {
-        TvMass m = {0.0, 0.0, 0.0};
-        float nearest = INFINITY;
-        for (int v = wa + lane; v < wb; v += 32) {
-            float sv8[VEC];
-            float ab = 0.f, ss = 0.f, qs = 0.f;
-            if (!again) pair_vec<DT>(row_vec<DT, RES>(sp, v), row_vec<DT, RES>(sq, v), ref, c, false, sv8, ab, ss, qs, nearest);
-            else pair_vec<DT>(row_vec<DT, false>(mp, v), row_vec<DT, false>(mq, v), ref, c, true, sv8, ab, ss, qs, nearest);
-            m.absum += (double)ab; m.signed_q += (double)ss; m.q += (double)qs;
-            if (RES) {
-                if (DT == 1) *reinterpret_cast<float4*>(smem + (size_t)v * 16) = make_float4(sv8[0], sv8[1], sv8[2], sv8[3]);
-                *reinterpret_cast<float4*>(smem + (size_t)(sv + v) * 16) = make_float4(sv8[VEC - 4], sv8[VEC - 3], sv8[VEC - 2], sv8[VEC - 1]);
+                    for (int o = 16; o > 0; o >>= 1) moved += __shfl_xor_sync(0xffffffffu, moved, o);
+                    m.ss = (double)moved * 0x1p-43; m.near = __any_sync(0xffffffffu, m.near);
+                    m = meet(S.mass[1 + level], S.cta_mass[1 + level], m, C, rank, merge_mass);
+                    wide_too = m.near;
+                    if (!m.near || level == 1) { mass.ss += m.ss; break; }
+                }
             }
-        }
-        m.absum = warp_sum(m.absum); m.signed_q = warp_sum(m.signed_q); m.q = warp_sum(m.q);
-        const int near = __any_sync(0xffffffffu, nearest <= ref.near);
-        if (lane == 0) { S.mass[0][warp] = m.absum; S.mass[1][warp] = m.signed_q; S.mass[2][warp] = m.q; S.near[warp] = near; }
-        __syncthreads();
-        if (warp == 0) {
-            const int n = __any_sync(0xffffffffu, lane < nw && S.near[lane]);
-            double s[3];
-#pragma unroll
-            for (int i = 0; i < 3; ++i) s[i] = warp_sum(lane < nw ? S.mass[i][lane] : 0.0);
-            if (lane < C) {
-#pragma unroll
-                for (int i = 0; i < 3; ++i) st_remote(at_rank(&S.cta_mass[i][rank], lane), s[i]);
-                st_remote(at_rank(&S.cta_near[rank], lane), n);
+            // ... and, where even that leaves it open (equal rows, rows of one token, many ties), or FAR: around the rows' largest logits, pass 2 too.
+            if (wide_too) {
+                wide = true;
+                Ring<DT, 2> r2 = ring;
+                tv_exact<DT, true>(r2, S, left0, c, rank, C, tot);
+                ring = r2;
+                ref = pair_ref<true>(tot.p, tot.q, tau, 0.f);
+                s_ab = s_ss = s_qs = 0.0;
+                ring.pass_small(left0, false, nullptr, [&](int, const uint4* x, auto) { pair_vec<DT, true, true>(x[0], x[1], ref, c, A); }, [&](const unsigned char*, int) { spill(); });
+                open = 0;
+                mass = meet(S.mass[3], S.cta_mass[3], part(), C, rank, merge_mass);
             }
+            const double q = wide ? mass.q : tot.q.s;       // (wide: by the same terms' sum, so that S is 1 where no q is above p)
+            tv = fmin(fmax(0.5 * mass.ab / tot.p.s, 0.0), 1.0);
+            s_aux = fmin(fmax(0.5 * (mass.ss + q) / q, 0.0), 1.0);
+            scale = (double)g / ((double)tau * q);
         }
-        cluster_sync();
-        if (again || !__any_sync(0xffffffffu, lane < C && S.cta_near[lane])) break;
-        // ---- the sums in double, around the same references
-        double ds[2] = {0.0, 0.0};
-        for (int w = 0; w < 2; ++w)
-            for (int v = wa + lane; v < wb; v += 32) {
-                float f[VEC];
-                unpack<DT>(row_vec<DT, false>(w ? mq : mp, v), f);
-                const double m0 = (double)(w ? ref.mq : ref.mp);
+        if (first) {
+            if (a.tv) a.tv[u] = (float)tv;
+            if (a.s_aux) a.s_aux[u] = (float)s_aux;
+            if (a.row_status) a.row_status[u] = st;
+        }
+        // ---- pass 3
+        const float below = (float)(-scale * (1.0 - s_aux)), over = (float)(scale * s_aux);
+        const auto put = [&](int at, const float* o, auto whole) {
+            if (decltype(whole)::value) store_whole<DT>(grow + at, 0, o);
+            else if (at < ring.bytes) store_vec<DT>(grow, at >> 4, left0, o);
+        };
+        const unsigned char* const* const next = more ? next_at : nullptr;
+        if (st) ring.pass_small(left0, true, next, [&](int at, const uint4*, auto whole) {
+            float o[VEC];
 #pragma unroll
-                for (int i = 0; i < VEC; ++i) ds[w] += q_exp2(((double)f[i] - m0) * c.d, S.tab);
-            }
-        for (int w = 0; w < 2; ++w) { const double x = warp_sum(ds[w]); if (lane == 0) S.wsum[w][warp] = x; }
-        __syncthreads();
-        if (warp < 2) {
-            const double x = warp_sum(lane < nw ? S.wsum[warp][lane] : 0.0);
-            if (lane < C) st_remote(at_rank(&S.cta_sum[warp][rank], lane), x);
-        }
-        cluster_sync();
-        RSum xp = tp, xq = tq;
-        xp.s = warp_sum(lane < C ? S.cta_sum[0][lane] : 0.0);
-        xq.s = warp_sum(lane < C ? S.cta_sum[1][lane] : 0.0);
-        ref = pair_ref(xp, xq, c, tau);
-        again = true;
+            for (int i = 0; i < VEC; ++i) o[i] = 0.f;
+            put(at, o, whole);
+        }, NoHook());
+        else if (wide) ring.pass_small(left0, true, next, [&](int at, const uint4* x, auto whole) { float o[VEC]; grad_vec<DT, true, true>(x[0], x[1], ref, c, below, over, o); put(at, o, whole); }, NoHook());
+        else if (again) ring.pass_small(left0, true, next, [&](int at, const uint4* x, auto whole) { float o[VEC]; grad_vec<DT, false, true>(x[0], x[1], ref, c, below, over, o); put(at, o, whole); }, NoHook());
+        else ring.pass(left0, true, next, [&](int at, const uint4* x, auto whole) { float o[VEC]; grad_vec<DT, false, false>(x[0], x[1], ref, c, below, over, o); put(at, o, whole); }, NoHook());
     }
-    double absum = lane < C ? S.cta_mass[0][lane] : 0.0, signed_q = lane < C ? S.cta_mass[1][lane] : 0.0, q = lane < C ? S.cta_mass[2][lane] : 0.0;
-    absum = warp_sum(absum); signed_q = warp_sum(signed_q); q = warp_sum(q);
-    const double sum_p = tp.s, s_aux = fmin(fmax(0.5 * (signed_q + q) / q, 0.0), 1.0);      // (by the same terms' sum: 1 where no q is above p)
-    if (rank == 0 && tid == 0) {
-        if (a.tv) a.tv[b] = (float)fmin(fmax(0.5 * absum / sum_p, 0.0), 1.0);
-        if (a.s_aux) a.s_aux[b] = (float)s_aux;
-        if (a.row_status) a.row_status[b] = 0;
-    }
-    // ---- pass 3
-    const double scale = (double)g / ((double)tau * q);
-    const float below = (float)(-scale * (1.0 - s_aux)), above = (float)(-scale * s_aux);       // (times |q|; a negative q brings its own sign)
-    float nearest = 0.f;
-    for (int v = wa + lane; v < wb; v += 32) {
-        float s8[VEC], o[VEC];
-        if (RES) {
-            if (DT == 1) { const float4 x = *reinterpret_cast<const float4*>(smem + (size_t)v * 16); s8[0] = x.x; s8[1] = x.y; s8[2] = x.z; s8[3] = x.w; }
-            const float4 y = *reinterpret_cast<const float4*>(smem + (size_t)(sv + v) * 16);
-            s8[VEC - 4] = y.x; s8[VEC - 3] = y.y; s8[VEC - 2] = y.z; s8[VEC - 1] = y.w;
-        } else {
-            float ab = 0.f, ss = 0.f, qs = 0.f;
-            pair_vec<DT>(row_vec<DT, false>(mp, v), row_vec<DT, false>(mq, v), ref, c, again, s8, ab, ss, qs, nearest);
-        }
-        grad_vec<DT>(s8, below, above, o);
-        store_vec<DT>(grow, v0 + v, R.V, o);
-    }
+    if (C > 1) cluster_sync();                              // (nobody stores into a CTA that has left)
 }
 
 cudaError_t tv_grad(const RowArgs& r, const float* grad_tv, float* tv, float* s_aux, int32_t* row_status, void* grad, int64_t ld_grad,
@@ -249,10 +451,11 @@ cudaError_t tv_grad(const RowArgs& r, const float* grad_tv, float* tv, float* s_
     a.r = r; a.grad_tv = grad_tv; a.tv = tv; a.s_aux = s_aux; a.row_status = row_status;
     a.grad = static_cast<unsigned char*>(grad);
     a.g_row_bytes = ld_grad * (r.dt == 0 ? 4 : 2);
-    a.s = rows_shape(r.B, 2, r.nvec, stream_rows);
     a.expire = take_expire_wait() ? 1 : 0;
-    if (a.s.res) return r.dt == 0 ? rows_launch<k_tv_grad<0, true>>(a, r.B, a.s, stream) : rows_launch<k_tv_grad<1, true>>(a, r.B, a.s, stream);
-    return r.dt == 0 ? rows_launch<k_tv_grad<0, false>>(a, r.B, a.s, stream) : rows_launch<k_tv_grad<1, false>>(a, r.B, a.s, stream);
+    const auto none = [](int) { return 0; };
+    cudaError_t e = r.dt == 0 ? ring_shape<k_tv_grad<0>>(r.B, 2, r.nvec, TvRing0::BYTES, none, a.s) : ring_shape<k_tv_grad<1>>(r.B, 2, r.nvec, TvRing1::BYTES, none, a.s);
+    if (e != cudaSuccess) return e;
+    return r.dt == 0 ? ring_launch<k_tv_grad<0>>(a, a.s, stream) : ring_launch<k_tv_grad<1>>(a, a.s, stream);
 }
 
 }  // namespace bebop
