@@ -20,22 +20,24 @@ __device__ __noinline__ bool ring_wait_long(uint32_t bar, uint32_t parity) {
     return false;
 }
 
-// ROWS rows side by side; two slots of a chunk of each (one where a run is a single chunk).
-template <int DT, int ROWS> struct Ring {
-    static constexpr int VEC = Elem<DT>::VEC, PART = kRingChunk * 16, SLOT = ROWS * PART, BYTES = 2 * SLOT;      // bytes of a chunk of a row, of a slot, of a warp's ring
+// ROWS rows side by side; SLOTS slots of a chunk of each (fewer where a run has fewer chunks).
+template <int DT, int ROWS, int SLOTS> struct Ring {
+    static constexpr int VEC = Elem<DT>::VEC, PART = kRingChunk * 16, SLOT = ROWS * PART, BYTES = SLOTS * SLOT;      // bytes of a chunk of a row, of a slot, of a warp's ring
     const unsigned char* buf;                 // the lane's place in it
-    uint32_t smem, bar;                       // the ring and its two barriers
+    uint32_t smem, bar;                       // the ring and its slots' barriers
     const unsigned char* at[ROWS];            // the warp's runs of the unit that is being asked for
     int bytes, off;                           // of a run; where the next chunk to ask for begins
-    uint32_t two, ask_slot, take_slot, phase;
-    bool edge, failed;                        // the row ends inside the run's last vector
+    uint32_t slots, ask_slot, take_slot, phase;
+    int full;                                 // rows of 32 vectors, one a lane, that lie inside the run and the vocabulary: all but the last, perhaps
+    bool failed;
 
     __device__ __forceinline__ void init(unsigned char* b, unsigned long long* s, int len, int left0) {
         buf = b + (threadIdx.x & 31) * 16; smem = smem_u32(b); bar = smem_u32(s);
-        bytes = len * 16; off = 0; two = len > kRingChunk; ask_slot = take_slot = phase = 0; failed = false;
-        edge = left0 < len * VEC;
+        bytes = len * 16; off = 0; slots = max(1, min(SLOTS, (len + kRingChunk - 1) / kRingChunk)); ask_slot = take_slot = phase = 0; failed = false;
+        full = (left0 < len * VEC ? len - 1 : len) / 32;
         if ((threadIdx.x & 31) == 0) {
-            mbar_init(&s[0], 1); mbar_init(&s[1], 1);
+#pragma unroll
+            for (int i = 0; i < SLOTS; ++i) mbar_init(&s[i], 1);
             asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         }
         __syncwarp();
@@ -50,23 +52,22 @@ template <int DT, int ROWS> struct Ring {
             for (int r = 0; r < ROWS; ++r)
                 asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" :: "r"(to + r * PART), "l"(at[r] + off), "r"(n), "r"(b) : "memory");
         }
-        ask_slot ^= two;
+        if (++ask_slot == slots) ask_slot = 0;
         off = off + PART >= bytes ? 0 : off + PART;
     }
-    __device__ __forceinline__ void first() { if (bytes > 0) ask(); if (two) ask(); }
-    // One pass, by whole warps: f(the lane's first vector of a chunk, in shared memory; its bytes from the run's start; vectors of it a lane at least: kRingVecs, or 0 where it is
-    // the run's last and may end early).  `next`: where the next unit's run lies, if this is the unit's last pass (and there is one), else null.
+    __device__ __forceinline__ void first() { if (bytes > 0) for (uint32_t i = 0; i < slots; ++i) ask(); }
+    // One pass, by whole warps: f(the lane's first vector of a chunk, in shared memory; its bytes from the run's start; how many full rows it has, and whether another, in part).  `next`: where the next unit's run lies, if this is the unit's last pass (and there is one), else null.
     template <typename F> __device__ __forceinline__ void chunks_of(bool last, const unsigned char* const* next, F&& f) {
 #pragma unroll 1
         for (int rem = bytes; rem > 0; rem -= PART) {
             const uint32_t b = bar + 8 * take_slot;
             if (!mbar_try(b, phase) && !ring_wait_long(b, phase)) failed = true;
-            f(buf + take_slot * SLOT, bytes - rem, rem > PART || (rem == PART && !edge));
-            phase ^= take_slot | (two ^ 1);
-            take_slot ^= two;
+            const int from = bytes - rem, n = min(kRingVecs, full - from / 512);
+            f(buf + take_slot * SLOT, from, n, n < kRingVecs && rem > n * 512);
+            if (++take_slot == slots) { take_slot = 0; phase ^= 1; }
             __syncwarp();
             // the slot is free: the chunk one ring's length ahead, of this unit or, behind its last pass, of the next
-            if (!last || rem > (two ? 2 * PART : PART)) ask();
+            if (!last || rem > (int)slots * PART) ask();
             else if (next) {
                 if (off == 0)
 #pragma unroll
@@ -88,23 +89,24 @@ template <int DT, int ROWS> struct Ring {
     // `left0`: tokens of the vocabulary from the run's first on.
     template <typename F, typename G> __device__ __forceinline__ void pass(int left0, bool last, const unsigned char* const* next, F&& f, G&& g) {
         const int lane = threadIdx.x & 31;
-        chunks_of(last, next, [&](const unsigned char* b, int from, bool whole) {
-            if (whole) {
+        chunks_of(last, next, [&](const unsigned char* b, int from, int n, bool part) {
+            const auto row = [&](int j) {
+                uint4 x[ROWS];
 #pragma unroll
-                for (int j = 0; j < kRingVecs; ++j) {
-                    uint4 x[ROWS];
+                for (int r = 0; r < ROWS; ++r) x[r] = whole_vec(b, r, j);
+                f(from + (j * 32 + lane) * 16, x, Count<1>());
+            };
+            if (n == kRingVecs) {
 #pragma unroll
-                    for (int r = 0; r < ROWS; ++r) x[r] = whole_vec(b, r, j);
-                    f(from + (j * 32 + lane) * 16, x, Count<1>());
-                }
+                for (int j = 0; j < kRingVecs; ++j) row(j);
             } else {
-                const int rem = bytes - from, left = left0 - (from >> 4) * VEC;
-#pragma unroll 1
-                for (int j = 0; j < kRingVecs && j * 512 < rem; ++j) {
+#pragma unroll 2
+                for (int j = 0; j < n; ++j) row(j);
+                if (part) {
                     uint4 x[ROWS];
 #pragma unroll
-                    for (int r = 0; r < ROWS; ++r) x[r] = edge_vec(b, r, j, rem, left);
-                    f(from + (j * 32 + lane) * 16, x, Count<0>());
+                    for (int r = 0; r < ROWS; ++r) x[r] = edge_vec(b, r, n, bytes - from, left0 - (from >> 4) * VEC);
+                    f(from + (n * 32 + lane) * 16, x, Count<0>());
                 }
             }
             g(b, from);
@@ -113,7 +115,7 @@ template <int DT, int ROWS> struct Ring {
     // ... the same for what is seldom called: a small loop (its instructions come from memory first, by the 128 bytes; six vectors' worth of them cost 25 us, this 2)
     template <typename F, typename G> __device__ __forceinline__ void pass_small(int left0, bool last, const unsigned char* const* next, F&& f, G&& g) {
         const int lane = threadIdx.x & 31;
-        chunks_of(last, next, [&](const unsigned char* b, int from, bool) {
+        chunks_of(last, next, [&](const unsigned char* b, int from, int, bool) {
             const int rem = bytes - from, left = left0 - (from >> 4) * VEC;
 #pragma unroll 1
             for (int j = 0; j < kRingVecs && j * 512 < rem; ++j) {
@@ -127,12 +129,13 @@ template <int DT, int ROWS> struct Ring {
     }
     // A pass for the rows' softmax sums: around the exponent of the warp's largest logit so far, a chunk's (at the end of a run a vector's) tokens in fp32, those in double.
     struct Sum { double s, s2; int e; float ef, top; bool bad; };      // (s2: of the squares)
-    template <bool LOW, bool SQUARES> __device__ __forceinline__ void sums(int left0, bool last, const unsigned char* const* next, const RScale& c, Sum* o) {
+    // h(the lane's place in a chunk, its bytes from the run's start) sees every chunk first, and may change the lane's own vectors of it.
+    template <bool LOW, bool SQUARES, typename H> __device__ __forceinline__ void sums(int left0, bool last, const unsigned char* const* next, const RScale& c, Sum* o, H&& h) {
 #pragma unroll
         for (int r = 0; r < ROWS; ++r) { o[r].s = o[r].s2 = 0.0; o[r].e = E_EMPTY; o[r].ef = 0.f; o[r].top = -INFINITY; o[r].bad = false; }
         const auto into = [&](Sum& a, const uint4* x, auto count) {
             constexpr int N = decltype(count)::value;
-            const float m = N > 1 ? vecs_max<DT, N>(x) : max_nan(vec_max<DT>(x[0]), -INFINITY);
+            const float m = vecs_max<DT, N>(x);
             if (!__all_sync(0xffffffffu, m <= a.top)) {       // (also a NaN; hardly ever after the first chunks)
                 const QExp E = chunk_exponent(m, c.c);
                 if (E.e == E_BAD) a.bad = true;
@@ -158,25 +161,32 @@ template <int DT, int ROWS> struct Ring {
             a.s += (double)((s0.x + s0.y) + (s1.x + s1.y));
             if (SQUARES) a.s2 += (double)(s2.x + s2.y);
         };
-        chunks_of(last, next, [&](const unsigned char* b, int from, bool whole) {
-            if (whole) {
+        chunks_of(last, next, [&](const unsigned char* b, int from, int n, bool part) {
+            h(b, from);
+            const auto rows = [&](int j0, auto count) {
 #pragma unroll
                 for (int r = 0; r < ROWS; ++r) {
-                    uint4 x[kRingVecs];
+                    uint4 x[decltype(count)::value];
 #pragma unroll
-                    for (int j = 0; j < kRingVecs; ++j) x[j] = whole_vec(b, r, j);
-                    into(o[r], x, Count<kRingVecs>());
+                    for (int j = 0; j < decltype(count)::value; ++j) x[j] = whole_vec(b, r, j0 + j);
+                    into(o[r], x, count);
                 }
-            } else {
-                const int rem = bytes - from, left = left0 - (from >> 4) * VEC;
+            };
+            if (n == kRingVecs) rows(0, Count<kRingVecs>());
+            else {
+                int j = 0;
 #pragma unroll 1
-                for (int j = 0; j < kRingVecs && j * 512 < rem; ++j)
+                for (; j + 2 <= n; j += 2) rows(j, Count<2>());
+                if (j < n) rows(j, Count<1>());
+                if (part)
 #pragma unroll
-                    for (int r = 0; r < ROWS; ++r) { const uint4 x = edge_vec(b, r, j, rem, left); into(o[r], &x, Count<1>()); }
+                    for (int r = 0; r < ROWS; ++r) { const uint4 x = edge_vec(b, r, n, bytes - from, left0 - (from >> 4) * VEC); into(o[r], &x, Count<1>()); }
             }
         });
     }
 };
+// the run of warp `warp` of nw, of nv vectors: whole rows of 32
+__device__ __forceinline__ int run_length(int nv, int nw) { return ((nv + 31) / 32 + nw - 1) / nw * 32; }
 
 // The warps' records, merged by a warp over its lanes (merge(records, n)), over the CTA and, through distributed shared memory, the cluster: the same in every
 // warp.  `warps` and `ctas` must not be in use any more; a second meeting takes others.
@@ -199,6 +209,26 @@ template <typename R, typename F> __device__ __forceinline__ R meet(R* warps, R*
     return merge(ctas, C);
 }
 
+// ... into the first warp alone.  (Nothing else of the cluster meets between two of these: `ctas` are taken in turn.)
+template <typename R, typename F> __device__ __forceinline__ R meet_first(R* warps, R* ctas, const R& mine, int C, int rank, F&& merge) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, nw = blockDim.x >> 5;
+    R r = mine;
+    if (lane == 0) warps[warp] = mine;
+    __syncthreads();
+    if (warp == 0) r = merge(warps, nw);
+    if (C == 1) return r;
+    if (warp == 0 && lane < C) {
+        const uint32_t d = at_rank(&ctas[rank], lane);
+        const int* const v = reinterpret_cast<const int*>(&r);
+#pragma unroll
+        for (int i = 0; i < (int)sizeof(R) / 4; ++i) st_remote(d + 4 * i, v[i]);
+    }
+    cluster_sync();
+    if (warp == 0) r = merge(ctas, C);
+    return r;
+}
+struct NoHook { __device__ __forceinline__ void operator()(const unsigned char*, int) const {} };
+
 struct RingShape { int C, sv, threads, clusters, bytes; };      // CTAs per unit, vectors per slice, threads, clusters of the grid, dynamic shared memory
 
 // How many CTAs (clusters) of a kernel the device holds at a time (asked once per device and shape; 0: not known).
@@ -219,8 +249,8 @@ template <auto kernel> int ring_resident(int C, int threads, int bytes) {
     return got > 0 ? got : 0;
 }
 
-// The cut of a call of `units` units of `held` rows of nvec vectors; `extra`: shared memory of a CTA beside the rings, for a slice of sv vectors.
-template <auto kernel, typename E> cudaError_t ring_shape(int units, int held, int nvec, int ring_bytes, E&& extra, RingShape& s) {
+// The cut of a call of `units` units of `held` rows of nvec vectors; `others`: warps of a CTA beside those with a ring; `extra`: shared memory of a CTA beside the rings, for a slice of sv vectors.
+template <auto kernel, typename E> cudaError_t ring_shape(int units, int held, int nvec, int ring_bytes, int others, E&& extra, RingShape& s) {
     const cudaError_t e = rows_ready<kernel>();
     if (e != cudaSuccess) return e;
     const int sms = rows_sms() > 0 ? rows_sms() : 148;
@@ -229,10 +259,13 @@ template <auto kernel, typename E> cudaError_t ring_shape(int units, int held, i
     // (the units under way at a time stay in L2 between their passes)
     while (s.C < kRowsMaxCluster && (double)sms / s.C * nvec * 16.0 * held > 96e6) ++s.C;
     s.sv = (nvec + s.C - 1) / s.C;
-    int warps = (s.sv + kRingChunk - 1) / kRingChunk;
-    warps = warps < 2 ? 2 : warps > kRingWarps ? kRingWarps : warps;
+    // Where there are more units than SMs, warps with seven chunks each at least: short rows then share an SM, one's passes under another's meetings (1,024 rows of
+    // 32,000 bf16 logits, loss alone: 39 us with 3 warps each, 58 with 15).  Else a warp for every chunk (100 rows of 49,999 fp32 logits: 15 us with 15, 38 with 3).
+    const int chunks = units * s.C > sms ? 7 : 1;
+    int warps = (s.sv + chunks * kRingChunk - 1) / (chunks * kRingChunk);
+    warps = warps < 2 ? 2 : warps > kRingWarps - others ? kRingWarps - others : warps;
     for (;; --warps) {
-        s.threads = 32 * warps;
+        s.threads = 32 * (warps + others);
         s.bytes = warps * ring_bytes + extra(s.sv);
         if (s.bytes <= kRowsSmem || warps == 1) break;
     }

@@ -40,6 +40,8 @@ struct PairRef {
     double theta_d;           // theta
 };
 
+constexpr int kTvSlots = 2;
+template <int DT> using TvRing = Ring<DT, 2, kTvSlots>;
 struct __align__(16) TvSums { RSum p, q; double p2, q2; };      // (p2, q2: sums of squares)
 
 // How far theta may be off, in units of tau.  Sums in fp32: every term carries an error of the order of 2^-24 (ex2.approx's bound is 2^-22) and of either sign, so
@@ -128,7 +130,7 @@ struct TvGradShared {
     TvMass mass[4][kRingWarps], cta_mass[4][kRowsMaxCluster];        // (pass 2, and three times more)
     TvTwo max[kRingWarps], cta_max[kRowsMaxCluster], exact[2][kRingWarps], cta_exact[2][kRowsMaxCluster];
     TvFour finer[kRingWarps], cta_finer[kRowsMaxCluster];
-    unsigned long long bar[kRingWarps][2];
+    unsigned long long bar[kRingWarps][kTvSlots];
     int opens;                                               // tokens whose comparison is open: how many, the first of them,
     unsigned long long open_mass;                            // what they weigh (2^-44), the smallest and the largest difference of their logits (ordered)
     long long open_least, open_most;
@@ -153,9 +155,6 @@ __device__ __forceinline__ TvMass merge_mass(const TvMass* s, int n) {
     return m;
 }
 
-struct NoHook { __device__ __forceinline__ void operator()(const unsigned char*, int) const {} };
-using TvRing0 = Ring<0, 2>;
-using TvRing1 = Ring<1, 2>;
 
 // 2^t of two numbers <= 1 in fp32 by the series of 2^f, |f| <= 1/2, to the seventh power (the next term is 5e-9 at most, 6e-10 in the mean): unlike ex2.approx's, its errors
 // are roundings without a mean that would stay in a sum of thousands.  Below -120: next to nothing.
@@ -177,17 +176,17 @@ __device__ __forceinline__ float2 series_exp2(float2 x, const RScale& c, float l
 // The sums of a row pair whose comparisons are open, more exactly: the terms from 2^-7 of the largest on in double, the others (most, and light) by the series above,
 // whose errors have no mean: of near_finer's bound, ten to forty times below near_fp32's, the largest error on the row pairs above is 0.47.  A fifth of tv_exact's time.
 constexpr float kTvHeavy = 0.0078125f;
-template <int DT> __device__ __noinline__ void tv_finer(Ring<DT, 2>& held, TvGradShared& S, int left0, const RScale& scale, int rank, int C, TvSums& tot) {
+template <int DT> __device__ __noinline__ void tv_finer(TvRing<DT>& held, TvGradShared& S, int left0, const RScale& scale, int rank, int C, TvSums& tot) {
     constexpr int VEC = Elem<DT>::VEC;
     const int lane = threadIdx.x & 31;
-    Ring<DT, 2> ring = held;
+    TvRing<DT> ring = held;
     const RScale c = scale;
     const int down[2] = {(int)tot.p.m, (int)tot.q.m};
     const float least[2] = {(tot.p.m - 120.f) / c.hi, (tot.q.m - 120.f) / c.hi};
     const float m[2] = {tot.p.m, tot.q.m};
     double d[2] = {0.0, 0.0};
     float h2[2] = {0.f, 0.f};
-    ring.chunks_of(false, nullptr, [&](const unsigned char* at, int from, bool) {
+    ring.chunks_of(false, nullptr, [&](const unsigned char* at, int from, int, bool) {
         const int rem = ring.bytes - from, left = left0 - (from >> 4) * VEC;
 #pragma unroll 1
         for (int j = 0; j < kRingVecs && j * 512 < rem; ++j) {
@@ -195,7 +194,7 @@ template <int DT> __device__ __noinline__ void tv_finer(Ring<DT, 2>& held, TvGra
 #pragma unroll
             for (int w = 0; w < 2; ++w) {
                 float f[VEC];
-                unpack<DT>(Ring<DT, 2>::edge_vec(at, w, j, rem, left), f);
+                unpack<DT>(TvRing<DT>::edge_vec(at, w, j, rem, left), f);
                 float2 s = make_float2(0.f, 0.f);
 #pragma unroll
                 for (int i = 0; i < VEC; i += 2) {
@@ -209,7 +208,7 @@ template <int DT> __device__ __noinline__ void tv_finer(Ring<DT, 2>& held, TvGra
 #pragma unroll 1
             for (; heavy; heavy &= heavy - 1) {
                 const int i = __ffs(heavy) - 1, w = i / VEC;
-                const unsigned char* const z = at + w * Ring<DT, 2>::PART + j * 512 + (i % VEC) * (16 / VEC);
+                const unsigned char* const z = at + w * TvRing<DT>::PART + j * 512 + (i % VEC) * (16 / VEC);
                 const float f = DT == 0 ? *reinterpret_cast<const float*>(z) : __uint_as_float((unsigned)*reinterpret_cast<const unsigned short*>(z) << 16);
                 const double e = q_exp2(row_arg<false>(f, w ? m[1] : m[0], c), g_pow2_64);
                 const float e2 = (float)(e * e);
@@ -227,7 +226,7 @@ template <int DT> __device__ __noinline__ void tv_finer(Ring<DT, 2>& held, TvGra
 __device__ __forceinline__ float near_finer(const TvSums& t) { return 6e-9f + 4.f * 5.9604644775390625e-08f * ((float)(sqrt(t.p2) / t.p.s) + (float)(sqrt(t.q2) / t.q.s)); }
 
 // ... and all of them in double.  FAR: around the rows' largest logits, which are found first.
-template <int DT, bool FAR> __device__ __noinline__ void tv_exact(Ring<DT, 2>& ring, TvGradShared& S, int left0, const RScale& c, int rank, int C, TvSums& tot) {
+template <int DT, bool FAR> __device__ __noinline__ void tv_exact(TvRing<DT>& ring, TvGradShared& S, int left0, const RScale& c, int rank, int C, TvSums& tot) {
     constexpr int VEC = Elem<DT>::VEC;
     const int lane = threadIdx.x & 31;
     if (FAR) {
@@ -265,7 +264,7 @@ __device__ __forceinline__ long long dord(double x) { const long long b = __doub
 template <int DT> __device__ __noinline__ void tv_collect(TvGradShared& S, const unsigned char* b, int rem, int left, const PairRef& R, const RScale& c) {
     constexpr int VEC = Elem<DT>::VEC;
     for (int j = 0; j < kRingVecs && j * 512 < rem; ++j) {
-        const uint4 xp = Ring<DT, 2>::edge_vec(b, 0, j, rem, left), xq = Ring<DT, 2>::edge_vec(b, 1, j, rem, left);
+        const uint4 xp = TvRing<DT>::edge_vec(b, 0, j, rem, left), xq = TvRing<DT>::edge_vec(b, 1, j, rem, left);
         float eq[VEC], fp[VEC], fq[VEC];
         row_exp<DT, DT == 0, false>(xq, R.mq, c, eq);
         unpack<DT>(xp, fp); unpack<DT>(xq, fq);
@@ -296,10 +295,10 @@ __global__ void __launch_bounds__(32 * kRingWarps, 1) k_tv_grad(const __grid_con
     const int C = a.s.C, sv = a.s.sv;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, nw = blockDim.x >> 5;
     const int rank = (int)cluster_rank(), clusters = a.s.clusters;
-    const int v0 = rank * sv, nv = max(min(sv, R.nvec - v0), 0), per = (nv + nw - 1) / nw, wa = min(warp * per, nv), len = min(per, nv - wa);
+    const int v0 = rank * sv, nv = max(min(sv, R.nvec - v0), 0), per = run_length(nv, nw), wa = min(warp * per, nv), len = min(per, nv - wa);
     const int left0 = R.V - (v0 + wa) * VEC;                // tokens from the warp's first vector on
-    Ring<DT, 2> ring;
-    ring.init(smem + (size_t)warp * Ring<DT, 2>::BYTES, S.bar[warp], len, left0);
+    TvRing<DT> ring;
+    ring.init(smem + (size_t)warp * TvRing<DT>::BYTES, S.bar[warp], len, left0);
     // (programmatic dependent launch: nothing of the caller's memory is touched until the grid before this one is through)
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
@@ -318,8 +317,8 @@ __global__ void __launch_bounds__(32 * kRingWarps, 1) k_tv_grad(const __grid_con
         unsigned char* const grow = a.grad + (int64_t)u * a.g_row_bytes + (int64_t)(v0 + wa) * 16;      // the warp's run of the gradient
         const bool first = rank == 0 && threadIdx.x == 0;
         // ---- pass 1
-        typename Ring<DT, 2>::Sum rs[2];
-        ring.template sums<DT == 0, true>(left0, false, nullptr, c, rs);
+        typename TvRing<DT>::Sum rs[2];
+        ring.template sums<DT == 0, true>(left0, false, nullptr, c, rs, NoHook());
         TvSums tot;
         tot.p.s = warp_sum(rs[0].s); tot.q.s = warp_sum(rs[1].s); tot.p2 = warp_sum(rs[0].s2); tot.q2 = warp_sum(rs[1].s2);
         tot.p.m = rs[0].e == E_EMPTY ? -INFINITY : (float)rs[0].e; tot.q.m = rs[1].e == E_EMPTY ? -INFINITY : (float)rs[1].e;
@@ -375,7 +374,7 @@ __global__ void __launch_bounds__(32 * kRingWarps, 1) k_tv_grad(const __grid_con
             if (again && !far) {
                 const float near = ref.near;
                 for (int level = 0; level < 2; ++level) {
-                    Ring<DT, 2> r2 = ring;                  // (by a copy, so that the ring itself stays in registers)
+                    TvRing<DT> r2 = ring;                  // (by a copy, so that the ring itself stays in registers)
                     TvSums exact = tot;
                     if (level == 0) tv_finer<DT>(r2, S, left0, c, rank, C, exact); else tv_exact<DT, false>(r2, S, left0, c, rank, C, exact);
                     ring = r2;
@@ -406,7 +405,7 @@ __global__ void __launch_bounds__(32 * kRingWarps, 1) k_tv_grad(const __grid_con
             // ... and, where even that leaves it open (equal rows, rows of one token, many ties), or FAR: around the rows' largest logits, pass 2 too.
             if (wide_too) {
                 wide = true;
-                Ring<DT, 2> r2 = ring;
+                TvRing<DT> r2 = ring;
                 tv_exact<DT, true>(r2, S, left0, c, rank, C, tot);
                 ring = r2;
                 ref = pair_ref<true>(tot.p, tot.q, tau, 0.f);
@@ -453,7 +452,7 @@ cudaError_t tv_grad(const RowArgs& r, const float* grad_tv, float* tv, float* s_
     a.g_row_bytes = ld_grad * (r.dt == 0 ? 4 : 2);
     a.expire = take_expire_wait() ? 1 : 0;
     const auto none = [](int) { return 0; };
-    cudaError_t e = r.dt == 0 ? ring_shape<k_tv_grad<0>>(r.B, 2, r.nvec, TvRing0::BYTES, none, a.s) : ring_shape<k_tv_grad<1>>(r.B, 2, r.nvec, TvRing1::BYTES, none, a.s);
+    cudaError_t e = r.dt == 0 ? ring_shape<k_tv_grad<0>>(r.B, 2, r.nvec, TvRing<0>::BYTES, 0, none, a.s) : ring_shape<k_tv_grad<1>>(r.B, 2, r.nvec, TvRing<1>::BYTES, 0, none, a.s);
     if (e != cudaSuccess) return e;
     return r.dt == 0 ? ring_launch<k_tv_grad<0>>(a, a.s, stream) : ring_launch<k_tv_grad<1>>(a, a.s, stream);
 }
