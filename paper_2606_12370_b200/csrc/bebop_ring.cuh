@@ -27,14 +27,24 @@ template <int DT, int ROWS, int SLOTS> struct Ring {
     uint32_t smem, bar;                       // the ring and its slots' barriers
     const unsigned char* at[ROWS];            // the warp's runs of the unit that is being asked for
     int bytes, off;                           // of a run; where the next chunk to ask for begins
-    uint32_t slots, ask_slot, take_slot, phase;
+    uint32_t slots, ask_slot, take_slot, phase;      // (phase: a bit for every slot)
     int full;                                 // rows of 32 vectors, one a lane, that lie inside the run and the vocabulary: all but the last, perhaps
     bool failed;
 
+    __device__ __forceinline__ void shape(int len, int left0) {
+        bytes = len * 16; off = 0; slots = max(1, min(SLOTS, (len + kRingChunk - 1) / kRingChunk)); ask_slot = take_slot = 0;
+        full = (left0 < len * VEC ? len - 1 : len) / 32;
+    }
+    // another run, once nothing is on its way any more
+    __device__ __forceinline__ void aim(const unsigned char* run, int len, int left0) {
+        shape(len, left0);
+        at[0] = run;
+        first();
+    }
     __device__ __forceinline__ void init(unsigned char* b, unsigned long long* s, int len, int left0) {
         buf = b + (threadIdx.x & 31) * 16; smem = smem_u32(b); bar = smem_u32(s);
-        bytes = len * 16; off = 0; slots = max(1, min(SLOTS, (len + kRingChunk - 1) / kRingChunk)); ask_slot = take_slot = phase = 0; failed = false;
-        full = (left0 < len * VEC ? len - 1 : len) / 32;
+        phase = 0; failed = false;
+        shape(len, left0);
         if ((threadIdx.x & 31) == 0) {
 #pragma unroll
             for (int i = 0; i < SLOTS; ++i) mbar_init(&s[i], 1);
@@ -56,15 +66,28 @@ template <int DT, int ROWS, int SLOTS> struct Ring {
         off = off + PART >= bytes ? 0 : off + PART;
     }
     __device__ __forceinline__ void first() { if (bytes > 0) for (uint32_t i = 0; i < slots; ++i) ask(); }
+    // Waits for the chunks that nobody takes any more (asked for by a pass with `next`).
+    __device__ __forceinline__ void drain() {
+        if (bytes > 0)
+            for (uint32_t i = 0; i < slots; ++i) {
+                const uint32_t b = bar + 8 * take_slot;
+                const uint32_t parity = phase >> take_slot & 1u;
+                if (!mbar_try(b, parity)) ring_wait_long(b, parity);
+                phase ^= 1u << take_slot;
+                if (++take_slot == slots) take_slot = 0;
+            }
+    }
     // One pass, by whole warps: f(the lane's first vector of a chunk, in shared memory; its bytes from the run's start; how many full rows it has, and whether another, in part).  `next`: where the next unit's run lies, if this is the unit's last pass (and there is one), else null.
     template <typename F> __device__ __forceinline__ void chunks_of(bool last, const unsigned char* const* next, F&& f) {
 #pragma unroll 1
         for (int rem = bytes; rem > 0; rem -= PART) {
             const uint32_t b = bar + 8 * take_slot;
-            if (!mbar_try(b, phase) && !ring_wait_long(b, phase)) failed = true;
+            const uint32_t parity = phase >> take_slot & 1u;
+            if (!mbar_try(b, parity) && !ring_wait_long(b, parity)) failed = true;
             const int from = bytes - rem, n = min(kRingVecs, full - from / 512);
             f(buf + take_slot * SLOT, from, n, n < kRingVecs && rem > n * 512);
-            if (++take_slot == slots) { take_slot = 0; phase ^= 1; }
+            phase ^= 1u << take_slot;
+            if (++take_slot == slots) take_slot = 0;
             __syncwarp();
             // the slot is free: the chunk one ring's length ahead, of this unit or, behind its last pass, of the next
             if (!last || rem > (int)slots * PART) ask();

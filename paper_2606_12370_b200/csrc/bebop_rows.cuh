@@ -3,7 +3,7 @@
 //
 // A softmax sum is (m, s) with s = sum 2^(x c - m), c = log2(e) / tau: m is a whole number near the largest x c, so that sums are merged by exact
 // powers of two, and fma(x, c, -m) carries one rounding of a small number.  m is a reference, not the maximum: a warp keeps its first
-// chunk's and moves it when a chunk lies above it.  Rows whose largest |x c| lies beyond 2^22 -- nothing but a mask of -1e9 or of the type's lowest
+// chunk's and moves it when a chunk lies above it.  Rows whose largest |x c| lies beyond 4 million -- nothing but a mask of -1e9 or of the type's lowest
 // value, a temperature next to zero -- are FAR: they are evaluated once more with the difference in front, 2^((x - m) c), m a logit, which holds for
 // finite logits of any size and costs an addition per two logits more.
 #pragma once
@@ -36,7 +36,7 @@ __device__ __forceinline__ RScale rows_scale(float tau) {
 struct __align__(16) RSum { double s; float m; int bad; };      // bad: bit 0 a NaN or +inf, bit 1 a wait that gave up
 __device__ __forceinline__ RSum no_sum() { RSum r; r.s = 0.0; r.m = -INFINITY; r.bad = 0; return r; }
 
-constexpr float kRowsFar = 4194304.f, kRowsClamp = 1073741824.f;      // 2^22; references end at 2^30, far inside FAR
+constexpr float kRowsFar = (float)kFarExp, kRowsClamp = 1073741824.f;      // (where chunk_exponent ends; references end at 2^30, far inside FAR)
 __device__ __forceinline__ bool sum_far(float m) { return fabsf(m) >= kRowsFar && m > -INFINITY; }
 // the reference that a chunk's maximum gives: a logit (FAR), or a whole number, the power of two above the largest term
 template <bool FAR> __device__ __forceinline__ float row_ref(float m, const RScale& c) { return FAR ? m : ceilf(fminf(fmaxf(m * c.hi, -kRowsClamp), kRowsClamp)); }
@@ -81,6 +81,27 @@ __device__ __forceinline__ void row_exp(const uint4& raw, float m, const RScale&
         e[i + 1] = ex2f(t.y);
     }
 }
+
+__device__ __forceinline__ float2 minus2(float2 a, float2 b) { return __ffma2_rn(b, make_float2(-1.f, -1.f), a); }
+__device__ __forceinline__ float series_least(float m, const RScale& c) { return (m - 120.f) / c.hi; }
+// 2^(x c - m) of two logits in fp32, `down` = m, by the series of 2^f, |f| <= 1/2, to the seventh power (the next term is 5e-9 at most, 6e-10 in the mean): unlike ex2.approx's, its errors
+// are roundings without a mean that would stay in a sum of thousands.  Logits below `least` count as that: next to nothing.
+__device__ __forceinline__ float2 series_exp2(float2 x, const RScale& c, float least, int down) {
+    // x c = n + f first, f exactly but for 2^-26: the exponent loses nothing to the size of x c - m
+    const float2 magic = make_float2(12582912.f, 12582912.f), hi = make_float2(c.hi, c.hi), lo = make_float2(c.lo, c.lo);
+    x.x = fmaxf(x.x, least); x.y = fmaxf(x.y, least);
+    const float2 r = __ffma2_rn(x, hi, magic), f = __ffma2_rn(x, lo, __ffma2_rn(x, hi, minus2(magic, r)));
+    const auto k = [](float a) { return make_float2(a, a); };
+    float2 p = __ffma2_rn(f, k(1.5252734e-5f), k(1.5403530e-4f));      // ln2^7 / 7!, ln2^6 / 6!, ...
+    p = __ffma2_rn(f, p, k(1.3333558e-3f));
+    p = __ffma2_rn(f, p, k(9.6181291e-3f));
+    p = __ffma2_rn(f, p, k(5.5504109e-2f));
+    p = __ffma2_rn(f, p, k(2.4022651e-1f));
+    p = __ffma2_rn(f, p, k(6.9314718e-1f));
+    p = __ffma2_rn(f, p, k(1.f));
+    return make_float2(__int_as_float(__float_as_int(p.x) + ((__float_as_int(r.x) - down) << 23)), __int_as_float(__float_as_int(p.y) + ((__float_as_int(r.y) - down) << 23)));
+}
+constexpr float kHeavy = 0.0078125f;           // terms from here on are taken in double beside the series
 
 // Sum over a warp of numbers >= 0 (the same bits in every lane), exact to 2^-24 of each and 2^-40 of the largest: a power of two takes the largest into [1, 2),
 // then they are added as integers.  A tenth of the latency of five steps of double shuffles and additions.

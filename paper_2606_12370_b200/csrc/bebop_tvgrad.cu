@@ -70,7 +70,6 @@ __device__ __forceinline__ float min3_abs(float a, float b, float c) {      // o
     float d; asm("min.abs.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c)); return d;
 }
 __device__ __forceinline__ float sign_of(float u) { return __uint_as_float(0x3f800000u | (__float_as_uint(u) & 0x80000000u)); }      // 1 or -1
-__device__ __forceinline__ float2 minus2(float2 a, float2 b) { return __ffma2_rn(b, make_float2(-1.f, -1.f), a); }
 
 // z_p - z_q - theta of two tokens (NaN: masked in both rows, q = 0).  EXACT: distances below `near` in double; FAR: all of them, and each logit less its row's
 // largest first, as their difference may have no room for theta.
@@ -156,33 +155,15 @@ __device__ __forceinline__ TvMass merge_mass(const TvMass* s, int n) {
 }
 
 
-// 2^t of two numbers <= 1 in fp32 by the series of 2^f, |f| <= 1/2, to the seventh power (the next term is 5e-9 at most, 6e-10 in the mean): unlike ex2.approx's, its errors
-// are roundings without a mean that would stay in a sum of thousands.  Below -120: next to nothing.
-__device__ __forceinline__ float2 series_exp2(float2 x, const RScale& c, float least, int down) {
-    // x c = n + f first, f exactly but for 2^-26: the exponent loses nothing to the size of x c - m
-    const float2 magic = make_float2(12582912.f, 12582912.f), hi = make_float2(c.hi, c.hi), lo = make_float2(c.lo, c.lo);
-    x.x = fmaxf(x.x, least); x.y = fmaxf(x.y, least);
-    const float2 r = __ffma2_rn(x, hi, magic), f = __ffma2_rn(x, lo, __ffma2_rn(x, hi, minus2(magic, r)));
-    const auto k = [](float a) { return make_float2(a, a); };
-    float2 p = __ffma2_rn(f, k(1.5252734e-5f), k(1.5403530e-4f));      // ln2^7 / 7!, ln2^6 / 6!, ...
-    p = __ffma2_rn(f, p, k(1.3333558e-3f));
-    p = __ffma2_rn(f, p, k(9.6181291e-3f));
-    p = __ffma2_rn(f, p, k(5.5504109e-2f));
-    p = __ffma2_rn(f, p, k(2.4022651e-1f));
-    p = __ffma2_rn(f, p, k(6.9314718e-1f));
-    p = __ffma2_rn(f, p, k(1.f));
-    return make_float2(__int_as_float(__float_as_int(p.x) + ((__float_as_int(r.x) - down) << 23)), __int_as_float(__float_as_int(p.y) + ((__float_as_int(r.y) - down) << 23)));
-}
 // The sums of a row pair whose comparisons are open, more exactly: the terms from 2^-7 of the largest on in double, the others (most, and light) by the series above,
 // whose errors have no mean: of near_finer's bound, ten to forty times below near_fp32's, the largest error on the row pairs above is 0.47.  A fifth of tv_exact's time.
-constexpr float kTvHeavy = 0.0078125f;
 template <int DT> __device__ __noinline__ void tv_finer(TvRing<DT>& held, TvGradShared& S, int left0, const RScale& scale, int rank, int C, TvSums& tot) {
     constexpr int VEC = Elem<DT>::VEC;
     const int lane = threadIdx.x & 31;
     TvRing<DT> ring = held;
     const RScale c = scale;
     const int down[2] = {(int)tot.p.m, (int)tot.q.m};
-    const float least[2] = {(tot.p.m - 120.f) / c.hi, (tot.q.m - 120.f) / c.hi};
+    const float least[2] = {series_least(tot.p.m, c), series_least(tot.q.m, c)};
     const float m[2] = {tot.p.m, tot.q.m};
     double d[2] = {0.0, 0.0};
     float h2[2] = {0.f, 0.f};
@@ -199,8 +180,8 @@ template <int DT> __device__ __noinline__ void tv_finer(TvRing<DT>& held, TvGrad
 #pragma unroll
                 for (int i = 0; i < VEC; i += 2) {
                     float2 e = series_exp2(make_float2(f[i], f[i + 1]), c, least[w], down[w]);
-                    if (e.x >= kTvHeavy) { heavy |= 1u << (w * VEC + i); e.x = 0.f; }
-                    if (e.y >= kTvHeavy) { heavy |= 2u << (w * VEC + i); e.y = 0.f; }
+                    if (e.x >= kHeavy) { heavy |= 1u << (w * VEC + i); e.x = 0.f; }
+                    if (e.y >= kHeavy) { heavy |= 2u << (w * VEC + i); e.y = 0.f; }
                     s = __fadd2_rn(s, e);
                 }
                 d[w] += (double)(s.x + s.y);
