@@ -238,7 +238,7 @@ bebop_status_t bebop_distill(
  * split-row general kernels for shapes none of them takes; 1 the general kernels always; 2 the pipelined kernel
  * wherever it applies; 3 the fused kernel wherever it applies (the greedy mode has no fused form); 4 the sequence kernel
  * wherever it applies.  All give the same results up to the documented tolerances.  (bebop_target_only_verify, bebop_tv_grad and
- * bebop_distill: with 1 they read their rows from memory in every pass, as they do for rows that sixteen SMs cannot hold.)  bebop_debug_last_kernel() says
+ * bebop_distill have one kernel each, whatever the mode.)  bebop_debug_last_kernel() says
  * what the last of these calls ran: 1 the general kernels, 2 the pipelined kernel, 3 the fused or the sequence
  * kernel (0: no call yet); bebop_debug_last_kernel_name() says it by name: "general", "k_pipe" (its sweeps, or with a TV
  * output the stream, k_fuse, under this name), "k_fuse", "k_seq", "k_seq_greedy" ("none": no call yet).

@@ -259,7 +259,7 @@ bebop_status_t bebop_target_only_verify(const void* target_logits, int64_t ld_ta
     if (!temperature && !(temperature_all > 0.f && temperature_all < INFINITY)) return BEBOP_ERR_TEMPERATURE;
     if ((s = check_arch()) != BEBOP_OK) return s;
     const RowArgs a = row_args(target_logits, ld_target, nullptr, 0, K + 1, K, draft_len, temperature, temperature_all, B, K, V, dt, whole_rows(V, dt));
-    const cudaError_t e = target_only(a, draft_tokens, u_accept, u_final, accept_len, out_tokens, p_draft, row_status, g_path == 1,
+    const cudaError_t e = target_only(a, draft_tokens, u_accept, u_final, accept_len, out_tokens, p_draft, row_status,
                                       static_cast<cudaStream_t>(cuda_stream));
     return e == cudaSuccess ? BEBOP_OK : BEBOP_ERR_CUDA;
 }
@@ -278,7 +278,7 @@ bebop_status_t bebop_tv_grad(const void* target_logits, int64_t ld_target, const
         return BEBOP_ERR_OVERLAP;
     if ((s = check_arch()) != BEBOP_OK) return s;
     const RowArgs a = row_args(target_logits, ld_target, draft_logits, ld_draft, 1, 1, nullptr, temperature, temperature_all, N, 1, V, dt, whole_rows(V, dt));
-    const cudaError_t e = tv_grad(a, grad_tv, tv, s_aux, row_status, grad_draft, ld_grad, g_path == 1, static_cast<cudaStream_t>(cuda_stream));
+    const cudaError_t e = tv_grad(a, grad_tv, tv, s_aux, row_status, grad_draft, ld_grad, static_cast<cudaStream_t>(cuda_stream));
     return e == cudaSuccess ? BEBOP_OK : BEBOP_ERR_CUDA;
 }
 
@@ -296,7 +296,7 @@ bebop_status_t bebop_distill(const void* draft_logits, int64_t ld_draft, const i
     if (grad_draft && rows_overlap(grad_draft, ld_grad, draft_logits, ld_draft, N, V, dt)) return BEBOP_ERR_OVERLAP;
     if ((s = check_arch()) != BEBOP_OK) return s;
     const RowArgs a = row_args(nullptr, 0, draft_logits, ld_draft, 1, 1, nullptr, temperature, temperature_all, N, 1, V, dt, whole_rows(V, dt));
-    const cudaError_t e = distill(a, top_ids, top_logits, (int)top_dt, T, target_lse, grad_loss, loss, row_status, grad_draft, ld_grad, g_path == 1,
+    const cudaError_t e = distill(a, top_ids, top_logits, (int)top_dt, T, target_lse, grad_loss, loss, row_status, grad_draft, ld_grad,
                                   static_cast<cudaStream_t>(cuda_stream));
     return e == cudaSuccess ? BEBOP_OK : BEBOP_ERR_CUDA;
 }

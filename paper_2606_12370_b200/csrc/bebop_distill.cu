@@ -122,29 +122,6 @@ enum { BAR_SUMS = 1, BAR_ROW, BAR_WRITTEN };                  // the readers' su
 // the bits of vector vi's tokens
 template <int DT> __device__ __forceinline__ uint32_t entry_bits(const unsigned char* bits, int vi) { return DT == 0 ? (bits[vi >> 1] >> ((vi & 1) * 4)) & 15u : bits[vi]; }
 
-// A warp's sum outside the entries around its largest logit, in double, of a row read from memory.
-template <int DT> __device__ __noinline__ void far_sum(const unsigned char* gz, int v0, int a, int b, int V, const unsigned char* bits, const RScale& c, double& s, float& m) {
-    constexpr int VEC = Elem<DT>::VEC;
-    const int lane = threadIdx.x & 31;
-    float top = -INFINITY;
-    double sum = 0.0;
-#pragma unroll 1
-    for (int pass = 0; pass < 2; ++pass) {
-#pragma unroll 1
-        for (int v = a + lane; v < b; v += 32) {
-            const uint32_t e = entry_bits<DT>(bits, v);
-            float f[VEC];
-            unpack<DT>(*reinterpret_cast<const uint4*>(gz + (size_t)v * 16), f);
-#pragma unroll
-            for (int i = 0; i < VEC; ++i)
-                if (!(e >> i & 1) && (v0 + v) * VEC + i < V) { if (pass == 0) top = fmaxf(top, f[i]); else sum += q_exp2(row_arg<true>(f[i], m, c), g_pow2_64); }
-        }
-        if (pass == 0) m = warp_max(top);
-        if (m == -INFINITY) break;
-    }
-    s = warp_sum(sum);
-}
-
 // What a CTA works on.
 template <int DT> struct DistillCta {
     const DistillArgs& a;
@@ -239,7 +216,7 @@ template <int DT> __device__ __forceinline__ void DistillCta<DT>::readers(unsign
         give(mine);
         const bool far = S.row.far;                         // (the same in every CTA)
         if (far) {
-            far_sum<DT>(draft(u) + (int64_t)v0 * 16, v0, wa, wa + len, R.V, my_bits, c, mine.s, mine.m);
+            mine = far_sum<DT>(Slice{draft(u) + (int64_t)v0 * 16, v0, nv, R.V}, wa, wa + len, c, [=](int v) { return entry_bits<DT>(my_bits, v); });
             give(mine);
         }
         if (!a.grad) continue;
@@ -428,7 +405,7 @@ __global__ void __launch_bounds__(32 * kRingWarps, 1) k_distill(const __grid_con
 }
 
 cudaError_t distill(const RowArgs& r, const int32_t* ids, const void* top, int top_dt, int T, const float* lse, const float* grad_loss, float* loss,
-                    int32_t* row_status, void* grad, int64_t ld_grad, bool stream_rows, cudaStream_t stream) {
+                    int32_t* row_status, void* grad, int64_t ld_grad, cudaStream_t stream) {
     DistillArgs a;
     a.r = r; a.ids = ids; a.top = top; a.top_dt = top_dt; a.T = T; a.lse = lse; a.grad_loss = grad_loss; a.loss = loss; a.row_status = row_status;
     a.grad = static_cast<unsigned char*>(grad);

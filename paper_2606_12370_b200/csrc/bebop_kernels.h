@@ -90,13 +90,13 @@ cudaError_t seq_greedy(const RowArgs& a, const int32_t* draft_tokens, int32_t* a
 cudaError_t pipe_greedy(const RowArgs& a, const Plan& p, const int32_t* draft_tokens, int32_t* accept_len,
                         int32_t* out_tokens, int32_t* row_status, char* ws, cudaStream_t stream, bool* launched);
 
-// The operators around a draft head: a cluster of CTAs per sequence, row pair or row, one launch, no workspace (bebop_rows.cuh has what they
-// share).  `stream_rows`: rows are read from memory by every pass, as for rows that do not fit the cluster's shared memory.
+// The operators around a draft head: a cluster of CTAs per sequence, row pair or row, one launch, no workspace (bebop_rows.cuh and
+// bebop_ring.cuh have what they share).
 cudaError_t target_only(const RowArgs& a, const int32_t* draft_tokens, const float* u_accept, const float* u_final, int32_t* accept_len, int32_t* out_tokens,
-                        float* p_draft, int32_t* row_status, bool stream_rows, cudaStream_t stream);
+                        float* p_draft, int32_t* row_status, cudaStream_t stream);
 cudaError_t tv_grad(const RowArgs& a, const float* grad_tv, float* tv, float* s_aux, int32_t* row_status, void* grad, int64_t ld_grad,
-                    bool stream_rows, cudaStream_t stream);
+                    cudaStream_t stream);
 cudaError_t distill(const RowArgs& a, const int32_t* ids, const void* top, int top_dt, int T, const float* lse, const float* grad_loss, float* loss,
-                    int32_t* row_status, void* grad, int64_t ld_grad, bool stream_rows, cudaStream_t stream);
+                    int32_t* row_status, void* grad, int64_t ld_grad, cudaStream_t stream);
 
 }  // namespace bebop

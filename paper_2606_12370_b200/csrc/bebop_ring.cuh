@@ -299,9 +299,7 @@ template <auto kernel, typename E> cudaError_t ring_shape(int units, int held, i
     return cudaSuccess;
 }
 template <auto kernel, typename A> cudaError_t ring_launch(const A& args, const RingShape& s, cudaStream_t stream) {
-    RowsShape r;
-    r.C = s.C; r.threads = s.threads; r.bytes = s.bytes; r.sv = s.sv; r.res = false;
-    return rows_launch<kernel>(args, s.clusters, r, stream);
+    return rows_launch<kernel>(args, s.clusters, s.C, s.threads, s.bytes, stream);
 }
 
 }  // namespace

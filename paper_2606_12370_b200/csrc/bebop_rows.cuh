@@ -1,9 +1,9 @@
-// What the kernels that take a row (a row pair) by a cluster of CTAs and need no other launch share: the slice of a row that a
-// CTA holds, its softmax sums, the exchange of the CTAs' sums, the launch.
+// What the kernels that take a row (a row pair) by a CTA or a cluster of them and need no other launch share: exponentials,
+// softmax sums and how they are merged, the launch.
 //
 // A softmax sum is (m, s) with s = sum 2^(x c - m), c = log2(e) / tau: m is a whole number near the largest x c, so that sums are merged by exact
-// powers of two, and fma(x, c, -m) carries one rounding of a small number.  m is a reference, not the maximum: a warp keeps its first
-// chunk's and moves it when a chunk lies above it.  Rows whose largest |x c| lies beyond 4 million -- nothing but a mask of -1e9 or of the type's lowest
+// powers of two, and fma(x, c, -m) carries one rounding of a small number.  m is a reference, not the maximum: the exponent
+// of the largest term, or of a larger one.  Rows whose largest |x c| lies beyond 4 million -- nothing but a mask of -1e9 or of the type's lowest
 // value, a temperature next to zero -- are FAR: they are evaluated once more with the difference in front, 2^((x - m) c), m a logit, which holds for
 // finite logits of any size and costs an addition per two logits more.
 #pragma once
@@ -13,13 +13,9 @@ namespace bebop {
 
 namespace {
 
-constexpr int RV = 4;                        // vectors per lane of a chunk
-constexpr int RCV = 32 * RV;                  // vectors per chunk
 constexpr int kRowsMaxCluster = 16;
-constexpr int kRowsMaxWarps = 8, kRowsMaxParts = kRowsMaxWarps * kRowsMaxCluster;
 constexpr int kRowsSmem = 232448 - 12288;     // dynamic shared memory of a CTA, at most (the rest: static tables)
 constexpr uint32_t kRowsSpin = 1u << 22;
-constexpr float kRowsSlack = 16.f;            // FAR: a sum's terms are at most 2^kRowsSlack (else 1)
 
 // log2(e) / tau, finite whatever tau, so that 0 * c is 0: to double precision (d), as the nearest float (c), and as a sum of floats hi + lo with lo
 // above 0, so that a masked logit's -inf stays -inf in both products.
@@ -36,10 +32,8 @@ __device__ __forceinline__ RScale rows_scale(float tau) {
 struct __align__(16) RSum { double s; float m; int bad; };      // bad: bit 0 a NaN or +inf, bit 1 a wait that gave up
 __device__ __forceinline__ RSum no_sum() { RSum r; r.s = 0.0; r.m = -INFINITY; r.bad = 0; return r; }
 
-constexpr float kRowsFar = (float)kFarExp, kRowsClamp = 1073741824.f;      // (where chunk_exponent ends; references end at 2^30, far inside FAR)
+constexpr float kRowsFar = (float)kFarExp;     // (where chunk_exponent ends)
 __device__ __forceinline__ bool sum_far(float m) { return fabsf(m) >= kRowsFar && m > -INFINITY; }
-// the reference that a chunk's maximum gives: a logit (FAR), or a whole number, the power of two above the largest term
-template <bool FAR> __device__ __forceinline__ float row_ref(float m, const RScale& c) { return FAR ? m : ceilf(fminf(fmaxf(m * c.hi, -kRowsClamp), kRowsClamp)); }
 // the factor that takes a sum around a to the reference b >= a; 0 where a is -inf
 template <bool FAR> __device__ __forceinline__ double ref_factor(float a, float b, const RScale& c) {
     if (FAR) return a == -INFINITY ? 0.0 : exp2(fmax(((double)a - (double)b) * c.d, -1100.0));
@@ -48,16 +42,16 @@ template <bool FAR> __device__ __forceinline__ double ref_factor(float a, float 
 // the exponent of logit x around reference m
 template <bool FAR> __device__ __forceinline__ double row_arg(float x, float m, const RScale& c) { return FAR ? ((double)x - (double)m) * c.d : fma((double)x, c.d, -(double)m); }
 
-// The slice of a row: vectors [v0, v0 + nv) of it, in shared memory (RES) or where the caller has them.
+// The slice of a row: vectors [v0, v0 + nv) of it, where the caller has them.
 struct Slice { const unsigned char* p; int v0, nv, V; };
 
 // vector vi of a slice; what lies beyond the slice or the vocabulary reads as -inf
-template <int DT, bool RES>
+template <int DT>
 __device__ __forceinline__ uint4 row_vec(const Slice& s, int vi) {
     constexpr int VEC = Elem<DT>::VEC;
     uint4 x = neg_inf_vec<DT>();
     if (vi < s.nv) {
-        x = RES ? *reinterpret_cast<const uint4*>(s.p + (size_t)vi * 16) : ldg16_stream(s.p + (size_t)vi * 16);
+        x = ldg16_stream(s.p + (size_t)vi * 16);
         const int left = s.V - (s.v0 + vi) * VEC;
         if (left < VEC) mask_tail<DT>(x, left);
     }
@@ -121,83 +115,34 @@ template <bool FAR> __device__ __forceinline__ RSum warp_merge(RSum r, const RSc
     return o;
 }
 
-// A chunk of RV vectors a lane into a warp's running sum, whose s differs by lane.
-template <int DT, bool LOW, bool FAR>
-__device__ __forceinline__ void chunk_into(RSum& r, const uint4* x, const RScale& c) {
+// A warp's sum of vectors [a, b) of a slice around its largest logit (FAR), in double, from memory; but for the tokens that `skip`, the bits of a vector, names.
+template <int DT, typename F> __device__ __noinline__ RSum far_sum(const Slice& sl, int a, int b, const RScale& c, F skip) {
     constexpr int VEC = Elem<DT>::VEC;
-    const float wm = ord2f(redux_max(f2ord(vecs_max<DT, RV>(x))));
-    if (!(wm < INFINITY)) { r.bad = 1; return; }
-    if (wm == -INFINITY) return;
-    const float m = row_ref<FAR>(wm, c);
-    if (FAR ? !((m - r.m) * c.hi <= kRowsSlack) : m > r.m) {      // (also: the first chunk with a logit)
-        r.s *= ref_factor<FAR>(r.m, m, c);
-        r.m = m;
-    }
-    float2 s0 = make_float2(0.f, 0.f), s1 = s0;
-#pragma unroll
-    for (int j = 0; j < RV; ++j) {
-        float e[VEC];
-        row_exp<DT, LOW, FAR>(x[j], r.m, c, e);
-#pragma unroll
-        for (int q = 0; q < VEC; q += 4) { s0 = __fadd2_rn(s0, make_float2(e[q], e[q + 1])); s1 = __fadd2_rn(s1, make_float2(e[q + 2], e[q + 3])); }
-    }
-    r.s += (double)((s0.x + s0.y) + (s1.x + s1.y));
-}
-
-// A warp's sum over vectors [a, b) of a slice: the lanes' parts in double, not yet added over the warp.  The vectors before `full` lie inside the vocabulary.
-template <int DT, bool RES, bool LOW, bool FAR>
-__device__ __forceinline__ RSum warp_row_sum(const Slice& sl, int a, int b, const RScale& c) {
     const int lane = threadIdx.x & 31;
+    float top = -INFINITY;
     RSum r = no_sum();
-    int v = a;
-    const int full = min(b, sl.V / Elem<DT>::VEC - sl.v0);
-    for (; v + RCV <= full; v += RCV) {
-        uint4 x[RV];
+#pragma unroll 1
+    for (int pass = 0; pass < 2; ++pass) {
+#pragma unroll 1
+        for (int v = a + lane; v < b; v += 32) {
+            const uint32_t e = skip(v);
+            float f[VEC];
+            unpack<DT>(row_vec<DT>(sl, v), f);
 #pragma unroll
-        for (int j = 0; j < RV; ++j) {
-            const unsigned char* const p = sl.p + (size_t)(v + j * 32 + lane) * 16;
-            x[j] = RES ? *reinterpret_cast<const uint4*>(p) : ldg16_stream(p);
+            for (int i = 0; i < VEC; ++i)
+                if (!(e >> i & 1)) { if (pass == 0) top = fmaxf(top, f[i]); else r.s += q_exp2(row_arg<true>(f[i], r.m, c), g_pow2_64); }
         }
-        chunk_into<DT, LOW, FAR>(r, x, c);
+        if (pass == 0) r.m = ord2f(redux_max(f2ord(top)));
+        if (r.m == -INFINITY) break;
     }
-    for (; v < b; v += RCV) {
-        uint4 x[RV];
-#pragma unroll
-        for (int j = 0; j < RV; ++j) { const int vi = v + j * 32 + lane; x[j] = vi < b ? row_vec<DT, RES>(sl, vi) : neg_inf_vec<DT>(); }
-        chunk_into<DT, LOW, FAR>(r, x, c);
-    }
+    r.s = warp_sum(r.s);
     return r;
-}
-
-// the warp's sum, added over its lanes
-__device__ __forceinline__ RSum warp_total(RSum r) { r.s = warp_sum_pos(r.s); return r; }
-// n sums, wherever they come from, as a lane's share of them: the entries lane, lane + 32, ... around the largest reference
-template <bool FAR> __device__ __forceinline__ RSum lane_share(const RSum* s, int n, const RScale& c) {
-    RSum r = no_sum();
-    for (int i = threadIdx.x & 31; i < n; i += 32) {
-        const RSum x = s[i];
-        const float m = fmaxf(r.m, x.m);
-        r.s = r.s * ref_factor<FAR>(r.m, m, c) + x.s * ref_factor<FAR>(x.m, m, c);
-        r.m = m; r.bad |= x.bad;
-    }
-    return r;
-}
-
-__device__ __forceinline__ void send_sum(RSum* at, const RSum& r, int rank) {
-    const uint32_t d = at_rank(at, rank);
-    st_remote(d, r.s); st_remote(d + 8, __float_as_int(r.m)); st_remote(d + 12, r.bad);
 }
 
 __device__ __forceinline__ int sum_status(const RSum& r) {
     if (r.bad & 2) return ST_WAIT;
     if (r.bad & 1) return ST_NONFINITE;
     return r.m == -INFINITY ? ST_EMPTY : 0;
-}
-
-__device__ __forceinline__ bool rows_wait(unsigned long long* b, uint32_t parity) {
-    const uint32_t addr = smem_u32(b);
-    for (uint32_t i = 0; i < kRowsSpin; ++i) { if (mbar_try(addr, parity)) return true; __nanosleep(32); }
-    return false;
 }
 
 // gradient vector `vi` of a row (in its own type) from floats
@@ -219,8 +164,6 @@ __device__ __forceinline__ void store_vec(unsigned char* row, int vi, int V, con
 }
 
 // ------------------------------------------------------------------ host
-struct RowsShape { int C, sv, bytes, threads; bool res; };      // CTAs per row, vectors per slice, dynamic shared memory, threads
-
 int rows_sms() {
     static int cached[64] = {0};
     int dev = 0, n = 0;
@@ -241,41 +184,19 @@ template <auto kernel> cudaError_t rows_ready() {
     if (dev >= 0 && dev < 64) done[dev] = true;
     return cudaSuccess;
 }
-template <auto kernel, typename A> cudaError_t rows_launch(const A& args, int rows, const RowsShape& s, cudaStream_t stream) {
+// `clusters` clusters of C CTAs
+template <auto kernel, typename A> cudaError_t rows_launch(const A& args, int clusters, int C, int threads, int bytes, cudaStream_t stream) {
     cudaError_t e = rows_ready<kernel>();
     if (e != cudaSuccess) return e;
     cudaLaunchAttribute attr[2];
     attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[1].val.programmaticStreamSerializationAllowed = 1;
     attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim.x = s.C; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
+    attr[0].val.clusterDim.x = C; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)rows * (unsigned)s.C); cfg.blockDim = dim3(s.threads); cfg.dynamicSmemBytes = s.bytes; cfg.stream = stream;
-    cfg.attrs = s.C == 1 ? attr + 1 : attr; cfg.numAttrs = s.C == 1 ? 1 : 2;      // (a plain grid starts sooner than one of clusters)
+    cfg.gridDim = dim3((unsigned)clusters * (unsigned)C); cfg.blockDim = dim3(threads); cfg.dynamicSmemBytes = bytes; cfg.stream = stream;
+    cfg.attrs = C == 1 ? attr + 1 : attr; cfg.numAttrs = C == 1 ? 1 : 2;      // (a plain grid starts sooner than one of clusters)
     return cudaLaunchKernelEx(&cfg, kernel, args);
-}
-
-// How a call's rows are cut: `held` row slices of a CTA side by side in shared memory, or, where sixteen CTAs cannot hold a row (or `stream` asks for
-// it), read from memory by every pass.  `extra` bytes and `bits` bits per vector are needed beside them.
-RowsShape rows_shape(int rows, int held, int nvec, bool stream, int extra = 0, int bits = 0) {
-    RowsShape s;
-    const int sms = rows_sms() > 0 ? rows_sms() : 148;
-    const auto slice = [&](int C) { return (nvec + C - 1) / C; };
-    const auto bytes = [&](int C) { return (long long)held * slice(C) * 16 + extra + (long long)slice(C) * bits / 8 + 8; };
-    s.res = !stream && bytes(kRowsMaxCluster) <= kRowsSmem;
-    s.C = kRowsMaxCluster;
-    if (s.res) {
-        constexpr int share = 72000;                         // (so that three CTAs share an SM)
-        s.C = 1;
-        while (s.C < kRowsMaxCluster && bytes(s.C) > share) ++s.C;
-        while (s.C < kRowsMaxCluster && (long long)rows * (s.C + 1) <= sms && (long long)held * nvec > (long long)s.C * 2048) ++s.C;
-    }
-    s.sv = slice(s.C);
-    s.bytes = s.res ? held * s.sv * 16 : 0;
-    int warps = (int)(((long long)held * s.sv + RCV - 1) / RCV);
-    warps = warps < 4 ? 4 : warps > kRowsMaxWarps ? kRowsMaxWarps : warps;
-    s.threads = 32 * warps;
-    return s;
 }
 
 }  // namespace

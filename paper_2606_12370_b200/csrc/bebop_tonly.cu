@@ -178,7 +178,7 @@ template <int DT, int LEVEL> __device__ __forceinline__ TonlyVerdict draw(TonlyS
                 int vi = -1;
 #pragma unroll 1
                 for (int v = b0; v < b1; v += 32) {
-                    const double s = vec_mass<DT, LEVEL>(v + lane < b1 ? row_vec<DT, false>(r.sl, v + lane) : neg_inf_vec<DT>(), v + lane, r, S.tab, m);
+                    const double s = vec_mass<DT, LEVEL>(v + lane < b1 ? row_vec<DT>(r.sl, v + lane) : neg_inf_vec<DT>(), v + lane, r, S.tab, m);
                     const int src = pick_lane(s, below, t, &base, &total, &hit);
                     if (src >= 0) {
                         vi = v + src; lo = base;
@@ -276,7 +276,7 @@ __global__ void __launch_bounds__(32 * kTonlyWarps, 1) k_target_only(const __gri
         sl.p = g;
         if (!tot.bad && sum_far(tot.m)) {
             far = true;
-            const RSum r = warp_total(warp_row_sum<DT, false, true, true>(sl, wa, wb, c));
+            const RSum r = far_sum<DT>(sl, wa, wb, c, [](int) { return 0u; });
             __syncthreads();                                // (every warp has read the sums that are written again now)
             if (C > 1) cluster_sync();
             tot = meet(S.sum[n & 1], S.cta_sum[n & 1], r, C, rank, [&](const RSum* s, int k) { return warp_merge<true>(lane < k ? s[lane] : no_sum(), c); });
@@ -304,7 +304,7 @@ __global__ void __launch_bounds__(32 * kTonlyWarps, 1) k_target_only(const __gri
         const int xv = row.x / VEC - v0;                    // the rejected draft's vector
         if (row.x >= 0 && xv >= wa && xv < wb) {            // (the warp's)
             float e[VEC];
-            row_exp<DT, true, false>(row_vec<DT, false>(sl, xv), tot.m, c, e);
+            row_exp<DT, true, false>(row_vec<DT>(sl, xv), tot.m, c, e);
 #pragma unroll
             for (int i = 0; i < VEC; ++i) if ((v0 + xv) * VEC + i == row.x) mass = fmax(mass - (double)e[i], 0.0);
         }
@@ -324,7 +324,7 @@ __global__ void __launch_bounds__(32 * kTonlyWarps, 1) k_target_only(const __gri
 }
 
 cudaError_t target_only(const RowArgs& r, const int32_t* draft_tokens, const float* u_accept, const float* u_final, int32_t* accept_len, int32_t* out_tokens,
-                        float* p_draft, int32_t* row_status, bool stream_rows, cudaStream_t stream) {
+                        float* p_draft, int32_t* row_status, cudaStream_t stream) {
     TonlyArgs a;
     a.r = r; a.draft_tokens = draft_tokens; a.u_accept = u_accept; a.u_final = u_final;
     a.accept_len = accept_len; a.out_tokens = out_tokens; a.p_draft = p_draft; a.row_status = row_status;

@@ -288,13 +288,16 @@ __global__ void __launch_bounds__(32 * kRingWarps, 1) k_tv_grad(const __grid_con
         at[1] = reinterpret_cast<const unsigned char*>(row_ptr(R, unit, R.K + 1)) + (int64_t)(v0 + wa) * 16;
     };
     int u = (int)(blockIdx.x / (unsigned)C);
+    float next_tau = tau_of(R, u), next_g = a.grad_tv ? a.grad_tv[u] : 1.f;
     run_at(u, ring.at);
     ring.first();
     if (C > 1) cluster_sync();                              // every CTA of the cluster has started
 #pragma unroll 1
     for (; u < R.B; u += clusters) {
-        const float tau = tau_of(R, u), g = a.grad_tv ? a.grad_tv[u] : 1.f;
+        const float tau = next_tau, g = next_g;
         const RScale c = rows_scale(tau);
+        const bool more = u + clusters < R.B;
+        if (more) { next_tau = tau_of(R, u + clusters); if (a.grad_tv) next_g = a.grad_tv[u + clusters]; }      // (asked for a row pair ahead)
         unsigned char* const grow = a.grad + (int64_t)u * a.g_row_bytes + (int64_t)(v0 + wa) * 16;      // the warp's run of the gradient
         const bool first = rank == 0 && threadIdx.x == 0;
         // ---- pass 1
@@ -316,7 +319,6 @@ __global__ void __launch_bounds__(32 * kRingWarps, 1) k_tv_grad(const __grid_con
         if (st & ST_WAIT) st = ST_WAIT;
         else if (!tau_ok(tau)) st = ST_BAD_TEMP;
         const unsigned char* next_at[2] = {nullptr, nullptr};
-        const bool more = u + clusters < R.B;
         if (more) run_at(u + clusters, next_at);
         PairRef ref = pair_ref<false>(tot.p, tot.q, tau, near_fp32(tot));
         double tv = 0.0, s_aux = 0.0, scale = 0.0;
@@ -426,7 +428,7 @@ __global__ void __launch_bounds__(32 * kRingWarps, 1) k_tv_grad(const __grid_con
 }
 
 cudaError_t tv_grad(const RowArgs& r, const float* grad_tv, float* tv, float* s_aux, int32_t* row_status, void* grad, int64_t ld_grad,
-                    bool stream_rows, cudaStream_t stream) {
+                    cudaStream_t stream) {
     TvGradArgs a;
     a.r = r; a.grad_tv = grad_tv; a.tv = tv; a.s_aux = s_aux; a.row_status = row_status;
     a.grad = static_cast<unsigned char*>(grad);
