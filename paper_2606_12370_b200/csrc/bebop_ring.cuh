@@ -30,6 +30,7 @@ template <int DT, int ROWS, int SLOTS> struct Ring {
     uint32_t slots, ask_slot, take_slot, phase;      // (phase: a bit for every slot)
     int full;                                 // rows of 32 vectors, one a lane, that lie inside the run and the vocabulary: all but the last, perhaps
     bool failed;
+    unsigned long long stays, gone;           // L2 policies
 
     __device__ __forceinline__ void shape(int len, int left0) {
         bytes = len * 16; off = 0; slots = max(1, min(SLOTS, (len + kRingChunk - 1) / kRingChunk)); ask_slot = take_slot = 0;
@@ -44,6 +45,8 @@ template <int DT, int ROWS, int SLOTS> struct Ring {
     __device__ __forceinline__ void init(unsigned char* b, unsigned long long* s, int len, int left0) {
         buf = b + (threadIdx.x & 31) * 16; smem = smem_u32(b); bar = smem_u32(s);
         phase = 0; failed = false;
+        asm volatile("createpolicy.fractional.L2::evict_normal.b64 %0, 1.0;" : "=l"(stays));
+        asm volatile("createpolicy.fractional.L2::evict_first.b64 %0, 1.0;" : "=l"(gone));
         shape(len, left0);
         if ((threadIdx.x & 31) == 0) {
 #pragma unroll
@@ -52,15 +55,17 @@ template <int DT, int ROWS, int SLOTS> struct Ring {
         }
         __syncwarp();
     }
-    // asks for the next chunk of the unit at `at`
-    __device__ __forceinline__ void ask() {
+    // asks for the next chunk of the unit at `at`.  `leave`: for the last time, so that its lines leave L2 first (768 row pairs of 151,936 bf16, 90 MB of them under way: 284 us
+    // without, 279 with; in clusters of two, half as many, 297 and 271).
+    __device__ __forceinline__ void ask(bool leave = false) {
         const int n = min(PART, bytes - off);
         if ((threadIdx.x & 31) == 0) {
             const uint32_t b = bar + 8 * ask_slot, to = smem + ask_slot * SLOT;
             asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" :: "r"(b), "r"(ROWS * n) : "memory");
 #pragma unroll
             for (int r = 0; r < ROWS; ++r)
-                asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" :: "r"(to + r * PART), "l"(at[r] + off), "r"(n), "r"(b) : "memory");
+                asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes.L2::cache_hint [%0], [%1], %2, [%3], %4;"
+                             :: "r"(to + r * PART), "l"(at[r] + off), "r"(n), "r"(b), "l"(leave ? gone : stays) : "memory");
         }
         if (++ask_slot == slots) ask_slot = 0;
         off = off + PART >= bytes ? 0 : off + PART;
@@ -90,7 +95,7 @@ template <int DT, int ROWS, int SLOTS> struct Ring {
             if (++take_slot == slots) take_slot = 0;
             __syncwarp();
             // the slot is free: the chunk one ring's length ahead, of this unit or, behind its last pass, of the next
-            if (!last || rem > (int)slots * PART) ask();
+            if (!last || rem > (int)slots * PART) ask(last);
             else if (next) {
                 if (off == 0)
 #pragma unroll
@@ -279,8 +284,8 @@ template <auto kernel, typename E> cudaError_t ring_shape(int units, int held, i
     const int sms = rows_sms() > 0 ? rows_sms() : 148;
     s.C = 1;
     while (s.C < kRowsMaxCluster && (long long)units * (s.C + 1) <= sms && nvec > s.C * 1024) ++s.C;
-    // (the units under way at a time stay in L2 between their passes)
-    while (s.C < kRowsMaxCluster && (double)sms / s.C * nvec * 16.0 * held > 96e6) ++s.C;
+    // (the units under way at a time stay in L2 between their passes: 90 MB of row pairs, read three times, came from DRAM 1.9 times)
+    while (s.C < kRowsMaxCluster && (double)sms / s.C * nvec * 16.0 * held > 80e6) ++s.C;
     s.sv = (nvec + s.C - 1) / s.C;
     // Where there are more units than SMs, warps with seven chunks each at least: short rows then share an SM, one's passes under another's meetings (1,024 rows of
     // 32,000 bf16 logits, loss alone: 39 us with 3 warps each, 58 with 15).  Else a warp for every chunk (100 rows of 49,999 fp32 logits: 15 us with 15, 38 with 3).
