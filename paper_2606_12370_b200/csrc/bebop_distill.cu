@@ -30,7 +30,9 @@ struct DistillArgs {
     unsigned char* grad;      // or nullptr
     int64_t g_row_bytes;
     int T, top_dt;
-    int o_tab, o_bits, words, marks;      // offsets in shared memory: two rows' entries; for two rows a bit for every token of the slice that is an entry, so many words, and a byte for every 32 vectors that hold one
+    // offsets in shared memory: two rows' entries; for two rows a bit for every token of the slice that is an entry, so many words, and a byte for every 32 vectors that hold one (the next row's
+    // `second` bytes behind: 0 where both do not fit, and a cluster takes one row)
+    int o_tab, o_bits, words, marks, second;
     RingShape s;
     int expire;
 };
@@ -394,8 +396,8 @@ __global__ void __launch_bounds__(32 * kRingWarps, 1) k_distill(const __grid_con
     extern __shared__ __align__(128) unsigned char smem[];
     __shared__ DistillShared S;
     const int rank = (int)cluster_rank(), nw = (blockDim.x >> 5) - 1, v0 = rank * a.s.sv;
-    DistillCta<DT> cta{a, S, {smem + a.o_bits, smem + a.o_bits + a.marks}, reinterpret_cast<int*>(smem + a.o_tab), rank, nw, v0, max(min(a.s.sv, a.r.nvec - v0), 0)};
-    for (int i = threadIdx.x; i < a.marks / 2; i += blockDim.x) reinterpret_cast<uint32_t*>(smem + a.o_bits)[i] = 0u;
+    DistillCta<DT> cta{a, S, {smem + a.o_bits, smem + a.o_bits + a.second}, reinterpret_cast<int*>(smem + a.o_tab), rank, nw, v0, max(min(a.s.sv, a.r.nvec - v0), 0)};
+    for (int i = threadIdx.x; i < (a.marks + a.second) / 4; i += blockDim.x) reinterpret_cast<uint32_t*>(smem + a.o_bits)[i] = 0u;
     // (programmatic dependent launch: nothing of the caller's memory is touched until the grid before this one is through)
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
@@ -415,11 +417,16 @@ cudaError_t distill(const RowArgs& r, const int32_t* ids, const void* top, int t
     // (a bit a token, of whole chunks beyond the slice: a lane looks at all of its chunk's vectors)
     const auto words = [=](int sv) { return ((sv + kRingChunk) * vec + 31) / 32; };
     const auto marks = [=](int sv) { return (4 * words(sv) + sv / 32 + kRingVecs + 16) & ~15; };
-    const auto extra = [=](int sv) { return 24 * T + 32 + 2 * marks(sv); };
     const int ring = DistillRing<0>::BYTES;
-    const cudaError_t e = r.dt == 0 ? ring_shape<k_distill<0>>(r.B, 1, r.nvec, ring, 1, extra, a.s) : ring_shape<k_distill<1>>(r.B, 1, r.nvec, ring, 1, extra, a.s);
+    const auto shape = [&](int rows) {
+        const auto extra = [=](int sv) { return 24 * T + 32 + rows * marks(sv); };
+        return r.dt == 0 ? ring_shape<k_distill<0>>(r.B, 1, r.nvec, ring, 1, extra, a.s) : ring_shape<k_distill<1>>(r.B, 1, r.nvec, ring, 1, extra, a.s);
+    };
+    cudaError_t e = shape(2);
+    const bool both = e == cudaSuccess;
+    if (e == cudaErrorInvalidConfiguration && (e = shape(1)) == cudaSuccess) a.s.clusters = r.B;      // (vocabularies beyond 10 million)
     if (e != cudaSuccess) return e;
-    a.o_tab = (a.s.threads / 32 - 1) * ring; a.o_bits = (a.o_tab + 24 * T + 15) & ~15; a.words = words(a.s.sv); a.marks = marks(a.s.sv);
+    a.o_tab = (a.s.threads / 32 - 1) * ring; a.o_bits = (a.o_tab + 24 * T + 15) & ~15; a.words = words(a.s.sv); a.marks = marks(a.s.sv); a.second = both ? a.marks : 0;
     return r.dt == 0 ? ring_launch<k_distill<0>>(a, a.s, stream) : ring_launch<k_distill<1>>(a, a.s, stream);
 }
 

@@ -289,7 +289,7 @@ template <auto kernel, typename E> cudaError_t ring_shape(int units, int held, i
     s.sv = (nvec + s.C - 1) / s.C;
     // Where there are more units than SMs, warps with seven chunks each at least: short rows then share an SM, one's passes under another's meetings (1,024 rows of
     // 32,000 bf16 logits, loss alone: 39 us with 3 warps each, 58 with 15).  Else a warp for every chunk (100 rows of 49,999 fp32 logits: 15 us with 15, 38 with 3).
-    const int chunks = units * s.C > sms ? 7 : 1;
+    const int chunks = (long long)units * s.C > sms ? 7 : 1;
     int warps = (s.sv + chunks * kRingChunk - 1) / (chunks * kRingChunk);
     warps = warps < 2 ? 2 : warps > kRingWarps - others ? kRingWarps - others : warps;
     for (;; --warps) {

@@ -306,7 +306,7 @@ __global__ void __launch_bounds__(32 * kRingWarps, 1) k_tv_grad(const __grid_con
         TvSums tot;
         tot.p.s = warp_sum(rs[0].s); tot.q.s = warp_sum(rs[1].s); tot.p2 = warp_sum(rs[0].s2); tot.q2 = warp_sum(rs[1].s2);
         tot.p.m = rs[0].e == E_EMPTY ? -INFINITY : (float)rs[0].e; tot.q.m = rs[1].e == E_EMPTY ? -INFINITY : (float)rs[1].e;
-        tot.p.bad = (rs[0].bad || rs[1].bad ? 1 : 0) | (a.expire || ring.failed ? 2 : 0); tot.q.bad = 0;
+        tot.p.bad = (rs[0].bad ? 1 : 0) | (a.expire || ring.failed ? 2 : 0); tot.q.bad = rs[1].bad ? 1 : 0;
         if (threadIdx.x == 0) { S.opens = 0; S.open_mass = 0; S.open_least = LLONG_MAX; S.open_most = LLONG_MIN; }                    // (nobody looks at the last unit's any more: a meeting lies behind)
         tot = meet(S.sum, S.cta_sum, tot, C, rank, [&](const TvSums* s, int n) {
             TvSums o, x;
