@@ -173,7 +173,8 @@ bebop_status_t bebop_greedy_verify(
  *   accept x_k while u_accept[b,k] < p_k(x_k); stop at the first reject
  *   at a reject at position n: draw y from p_n without x_n, renormalised; if all L accepted: from p_L
  *     y = min{ v : sum_{v'<=v} r(v') >= u_final[b] * sum r }
- * so that every emitted token is distributed as the target's.  Rows behind the stop are never read, and no anomaly in them is seen.
+ * so that every emitted token is distributed as the target's.  What the rows behind the stop hold does not matter, and no anomaly in
+ * them is seen (the first kilobytes of the next one may be loaded).
  * The accept test and the draw are decided as an fp64 evaluation decides them except on near-ties.
  * Arguments as in bebop_verify; p_draft [B,K] (may be NULL): p_k(x_k) of the positions read, 0 behind the stop.
  * BEBOP_ROW_ZERO_RESID: a draft of probability 1 was rejected (u_accept >= 1); the token is the draft.
@@ -249,7 +250,7 @@ bebop_status_t bebop_distill(
  * bebop_verify calls record around the main (pipelined or fused) kernel, on the caller's stream (NULL,
  * NULL switches it off).
  * bebop_debug_expire_wait(which): the next call's device-side wait number `which` (1: the re-draw kernel's wait
- * for the list of sequences; 2: the main kernel's wait for what other CTAs deliver; either: the three calls without a workspace) gives up at once, as if
+ * for the list of sequences; 2: the main kernel's wait for what other CTAs deliver; either: the waits of the three calls without a workspace for their rows) gives up at once, as if
  * its bound had run out: the call still returns, every row_status carries BEBOP_ROW_WAIT_EXPIRED, and the call
  * after it is normal again (0: off).  For the test of the bounded waits; nothing is trapped or hung.
  * bebop_debug_set_draw_kappa(kappa): the factor in the error bound that decides whether bebop_verify keeps a token
