@@ -284,14 +284,18 @@ template <auto kernel, typename E> cudaError_t ring_shape(int units, int held, i
     const int sms = rows_sms() > 0 ? rows_sms() : 148;
     s.C = 1;
     while (s.C < kRowsMaxCluster && (long long)units * (s.C + 1) <= sms && nvec > s.C * 1024) ++s.C;
-    // (the units under way at a time stay in L2 between their passes: 90 MB of row pairs, read three times, came from DRAM 1.9 times)
-    while (s.C < kRowsMaxCluster && (double)sms / s.C * nvec * 16.0 * held > 80e6) ++s.C;
+    // The units under way at a time stay in L2 between their passes (90 MB of row pairs, read three times, came from DRAM 1.9 times).  Where a unit to an SM is more than that, two CTAs share
+    // an SM, one's passes under the other's meetings, and a unit has as many as keeps them below (512 row pairs of 262,144 bf16: 326 us with four of 8 warps, 375 with two of 16, 415 with one).
+    const double mb = nvec * 16e-6 * held;
+    const bool two = sms / s.C * mb > 80.0;
+    while (two && s.C < kRowsMaxCluster && 2.0 * sms / s.C * mb > 95.0) ++s.C;
+    const int most = (two ? kRingWarps / 2 : kRingWarps) - others;
     s.sv = (nvec + s.C - 1) / s.C;
     // Where there are more units than SMs, warps with seven chunks each at least: short rows then share an SM, one's passes under another's meetings (1,024 rows of
     // 32,000 bf16 logits, loss alone: 39 us with 3 warps each, 58 with 15).  Else a warp for every chunk (100 rows of 49,999 fp32 logits: 15 us with 15, 38 with 3).
-    const int chunks = (long long)units * s.C > sms ? 7 : 1;
+    const int chunks = (long long)units * s.C > sms && !two ? 7 : 1;
     int warps = (s.sv + chunks * kRingChunk - 1) / (chunks * kRingChunk);
-    warps = warps < 2 ? 2 : warps > kRingWarps - others ? kRingWarps - others : warps;
+    warps = warps < 2 ? 2 : warps > most ? most : warps;
     for (;; --warps) {
         s.threads = 32 * (warps + others);
         s.bytes = warps * ring_bytes + extra(s.sv);
