@@ -12,6 +12,8 @@
 //   pass 2  the gradient, as of a row without entries; the entries' own is written behind it.
 // The entries are one warp's work, the keeper's, beside the readers': while they are in pass 1 of a row it gathers and sums that row's entries and sets the next
 // row's bits; between the passes it has the row's numbers; behind pass 2 it writes the entries' gradient.  The readers wait for it once a row.
+// 768 rows of 151,936 bf16, 64 entries: 118 us (0.61 of the copy rate; 134 with the entries spread over all warps), the loss alone 73; 100 rows of 49,999 fp32: 14.6, 12 of 1,024: 6.3.  The passes of a row lie one
+// after the other (DRAM reads, then writes), 14 instructions a logit at half the issue rate.
 #include "bebop_kernels.h"
 #include "bebop_ring.cuh"
 

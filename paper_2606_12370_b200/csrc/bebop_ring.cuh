@@ -259,13 +259,15 @@ struct NoHook { __device__ __forceinline__ void operator()(const unsigned char*,
 
 struct RingShape { int C, sv, threads, clusters, bytes; };      // CTAs per unit, vectors per slice, threads, clusters of the grid, dynamic shared memory
 
-// How many CTAs (clusters) of a kernel the device holds at a time (asked once per device and shape; 0: not known).
+// How many clusters of a kernel's CTAs the device holds at a time (asked once per device, cut and use of shared memory; 0: not known).
 template <auto kernel> int ring_resident(int C, int threads, int bytes) {
-    static int cached[64][kRowsMaxCluster + 1][kRingWarps + 1] = {{{0}}};
+    struct Held { int n, bytes; };
+    static Held cached[64][kRowsMaxCluster + 1][kRingWarps + 1] = {};
     int dev = 0;
     if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) { cudaGetLastError(); return 0; }
-    int& n = cached[dev][C][threads / 32];
-    if (n) return n > 0 ? n : 0;
+    Held& held = cached[dev][C][threads / 32];
+    const Held now = held;
+    if (now.n && now.bytes == bytes) return now.n > 0 ? now.n : 0;
     int got = 0;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeClusterDimension;
@@ -273,7 +275,7 @@ template <auto kernel> int ring_resident(int C, int threads, int bytes) {
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)C); cfg.blockDim = dim3(threads); cfg.dynamicSmemBytes = bytes; cfg.attrs = attr; cfg.numAttrs = 1;
     if (rows_ready<kernel>() != cudaSuccess || cudaOccupancyMaxActiveClusters(&got, kernel, &cfg) != cudaSuccess) { cudaGetLastError(); got = 0; }
-    n = got > 0 ? got : -1;
+    held = Held{got > 0 ? got : -1, bytes};
     return got > 0 ? got : 0;
 }
 
@@ -290,19 +292,23 @@ template <auto kernel, typename E> cudaError_t ring_shape(int units, int held, i
     const bool two = sms / s.C * mb > 80.0;
     while (two && s.C < kRowsMaxCluster && 2.0 * sms / s.C * mb > 95.0) ++s.C;
     const int most = (two ? kRingWarps / 2 : kRingWarps) - others;
-    s.sv = (nvec + s.C - 1) / s.C;
-    // Where there are more units than SMs, warps with seven chunks each at least: short rows then share an SM, one's passes under another's meetings (1,024 rows of
-    // 32,000 bf16 logits, loss alone: 39 us with 3 warps each, 58 with 15).  Else a warp for every chunk (100 rows of 49,999 fp32 logits: 15 us with 15, 38 with 3).
-    const int chunks = (long long)units * s.C > sms && !two ? 7 : 1;
-    int warps = (s.sv + chunks * kRingChunk - 1) / (chunks * kRingChunk);
-    warps = warps < 2 ? 2 : warps > most ? most : warps;
-    for (;; --warps) {
-        s.threads = 32 * (warps + others);
-        s.bytes = warps * ring_bytes + extra(s.sv);
-        if (s.bytes <= kRowsSmem || warps == 1) break;
+    for (;; --s.C) {
+        s.sv = (nvec + s.C - 1) / s.C;
+        // Where there are more units than SMs, warps with seven chunks each at least: short rows then share an SM, one's passes under another's meetings (1,024 rows of
+        // 32,000 bf16 logits, loss alone: 39 us with 3 warps each, 58 with 15).  Else a warp for every chunk (100 rows of 49,999 fp32 logits: 15 us with 15, 38 with 3).
+        const int chunks = (long long)units * s.C > sms && !two ? 7 : 1;
+        int warps = (s.sv + chunks * kRingChunk - 1) / (chunks * kRingChunk);
+        warps = warps < 2 ? 2 : warps > most ? most : warps;
+        for (;; --warps) {
+            s.threads = 32 * (warps + others);
+            s.bytes = warps * ring_bytes + extra(s.sv);
+            if (s.bytes <= kRowsSmem || warps == 1) break;
+        }
+        if (s.bytes > kRowsSmem) return cudaErrorInvalidConfiguration;
+        s.clusters = ring_resident<kernel>(s.C, s.threads, s.bytes);
+        // (few units: no larger clusters than the device holds at a time -- seven of sixteen, nine of fifteen)
+        if (s.clusters >= units || (long long)units * s.C > sms || s.C == 1) break;
     }
-    if (s.bytes > kRowsSmem) return cudaErrorInvalidConfiguration;
-    s.clusters = ring_resident<kernel>(s.C, s.threads, s.bytes);
     if (s.clusters <= 0) s.clusters = 1;
     if (s.clusters > units) s.clusters = units;
     return cudaSuccess;

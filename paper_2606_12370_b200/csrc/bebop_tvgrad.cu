@@ -11,8 +11,10 @@
 // A CTA (a cluster of them, where there are fewer row pairs than SMs or rows are long) takes a row pair three times: the first time from DRAM, then out of L2.
 //   pass 1  the rows' softmax sums
 //   pass 2  sum |p - q|, S, the smallest |z_p - z_q - theta|
-//   again   where that smallest distance is below the bound: sums in double, and pass 2 once more
+//   again   where that smallest distance is below the bound: the sums more exactly (33 us of the CTA's time at 151,936 tokens), by which the tokens that were open are decided
 //   pass 3  the gradient
+// 768 row pairs of 151,936 bf16: 272 us (0.39 of the copy rate; 256 where no comparison is open), 512 of 262,144: 306 to 325, 12 of 1,024 fp32: 6.0.  A row pair's 38 instructions a pair of logits and its
+// five exponentials bound it, with the meetings between passes; DRAM is busy in the first and the last pass.
 #include "bebop_kernels.h"
 #include "bebop_ring.cuh"
 
