@@ -4,10 +4,11 @@
 //   draw from p_n without x_n, else from the row behind the last draft: y = min{v : C(v) >= u_final C(V - 1)}
 //
 // The CTAs take the rows one after the other and stop where the sequence does; a row behind the stop is not read, but for the chunks that are on their way when
-// the row before it is rejected.  Several sequences share an SM, so that one's meetings lie under another's rows, and the hardware hands out the sequences.
+// the row before it is rejected.  The hardware hands out the sequences.
 // A warp owns a run of a row's vectors, in the order of the tokens, and leaves its sum, so that the draw goes from the CTAs' sums to the warps' and from there, over
 // the owner's run once more, to the tokens.  It is made with the fp32 exponentials of the sums; where their error could change the token, once more by the series of 2^f with what is heavy in
-// double (of 81,920 draws 2 % come to it), and in double (0.3 %).
+// double (2 % of the draws below come to it), and in double (0.3 %).  (The lanes' sums of every chunk kept for the draw, so that it reads one chunk again and not a run: 262 us for the 237 below, as the passes
+// pay for it.)
 // 1,024 sequences of up to five rows of 151,936 bf16: 237 us (0.45 of the copy rate; 170 without draws), 256 of four: 101 to 114, one: 13 to 18.  Sequences of different lengths and the draws that are left open bound
 // it; a step of the draw costs 25 to 80 us of its CTA's time.
 #include "bebop_kernels.h"
