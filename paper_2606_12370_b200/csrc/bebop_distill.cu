@@ -198,7 +198,7 @@ template <int DT> __device__ __forceinline__ void DistillCta<DT>::readers(unsign
         const unsigned char* const my_bits = bits[k];
         const unsigned char* const my_rows = my_bits + 4 * a.words;
         typename Rows::Sum rs[1];
-        ring.template sums<true, false>(left0, !a.grad, next, c, rs, [&](const unsigned char* b, int from) {
+        ring.template sums<true>(left0, !a.grad, next, c, rs, [&](const unsigned char* b, int from) {
             const int vi = wa + (from >> 4) + lane;
             uint32_t held = __ballot_sync(0xffffffffu, lane < kRingVecs && my_rows[(vi - lane) / 32 + lane]);      // the rows of 32 vectors that have entries
             if (held) {

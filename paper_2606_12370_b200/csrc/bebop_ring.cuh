@@ -156,11 +156,11 @@ template <int DT, int ROWS, int SLOTS> struct Ring {
         });
     }
     // A pass for the rows' softmax sums: around the exponent of the warp's largest logit so far, a chunk's (at the end of a run a vector's) tokens in fp32, those in double.
-    struct Sum { double s, s2; int e; float ef, top; bool bad; };      // (s2: of the squares)
+    struct Sum { double s; int e; float ef, top; bool bad; };
     // h(the lane's place in a chunk, its bytes from the run's start) sees every chunk first, and may change the lane's own vectors of it.
-    template <bool LOW, bool SQUARES, typename H> __device__ __forceinline__ void sums(int left0, bool last, const unsigned char* const* next, const RScale& c, Sum* o, H&& h) {
+    template <bool LOW, typename H> __device__ __forceinline__ void sums(int left0, bool last, const unsigned char* const* next, const RScale& c, Sum* o, H&& h) {
 #pragma unroll
-        for (int r = 0; r < ROWS; ++r) { o[r].s = o[r].s2 = 0.0; o[r].e = E_EMPTY; o[r].ef = 0.f; o[r].top = -INFINITY; o[r].bad = false; }
+        for (int r = 0; r < ROWS; ++r) { o[r].s = 0.0; o[r].e = E_EMPTY; o[r].ef = 0.f; o[r].top = -INFINITY; o[r].bad = false; }
         const auto into = [&](Sum& a, const uint4* x, auto count) {
             constexpr int N = decltype(count)::value;
             const float m = vecs_max<DT, N>(x);
@@ -168,26 +168,20 @@ template <int DT, int ROWS, int SLOTS> struct Ring {
                 const QExp E = chunk_exponent(m, c.c);
                 if (E.e == E_BAD) a.bad = true;
                 else if (E.e > a.e) {
-                    const double f = a.e == E_EMPTY ? 0.0 : pow2d(max(a.e - E.e, -500));
-                    a.s *= f; a.s2 *= f * f;
+                    a.s *= a.e == E_EMPTY ? 0.0 : pow2d(max(a.e - E.e, -500));
                     a.e = E.e; a.ef = E.ef;
                     a.top = (E.ef - 0.0625f) / c.c;           // (a margin beyond every rounding: what is not above it has x c <= e)
                 }
             }
-            float2 s0 = make_float2(0.f, 0.f), s1 = s0, s2 = s0;
+            float2 s0 = make_float2(0.f, 0.f), s1 = s0;
 #pragma unroll
             for (int j = 0; j < N; ++j) {
                 float e[VEC];
                 row_exp<DT, LOW, false>(x[j], a.ef, c, e);
 #pragma unroll
                 for (int q = 0; q < VEC; q += 4) { s0 = __fadd2_rn(s0, make_float2(e[q], e[q + 1])); s1 = __fadd2_rn(s1, make_float2(e[q + 2], e[q + 3])); }
-                if (SQUARES) {
-#pragma unroll
-                    for (int q = 0; q < VEC; q += 2) s2 = __ffma2_rn(make_float2(e[q], e[q + 1]), make_float2(e[q], e[q + 1]), s2);
-                }
             }
             a.s += (double)((s0.x + s0.y) + (s1.x + s1.y));
-            if (SQUARES) a.s2 += (double)(s2.x + s2.y);
         };
         chunks_of(last, next, [&](const unsigned char* b, int from, int n, bool part) {
             h(b, from);

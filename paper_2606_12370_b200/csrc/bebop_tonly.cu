@@ -271,7 +271,7 @@ __global__ void __launch_bounds__(32 * kTonlyWarps, 1) k_target_only(const __gri
         const unsigned char* next_at[1] = {nullptr};
         if (n < L) next_at[0] = reinterpret_cast<const unsigned char*>(row_ptr(R, b, n + 1)) + (int64_t)(v0 + wa) * 16;
         typename TonlyRing<DT>::Sum rs[1];
-        ring.template sums<true, false>(left0, true, n < L ? next_at : nullptr, c, rs, NoHook());
+        ring.template sums<true>(left0, true, n < L ? next_at : nullptr, c, rs, NoHook());
         asked = n < L;
         mine.s = warp_sum_pos(rs[0].s);
         mine.m = rs[0].e == E_EMPTY ? -INFINITY : (float)rs[0].e;

@@ -13,7 +13,7 @@
 //   pass 2  sum |p - q|, S, the smallest |z_p - z_q - theta|
 //   again   where that smallest distance is below the bound: the sums more exactly (33 us of the CTA's time at 151,936 tokens), by which the tokens that were open are decided
 //   pass 3  the gradient
-// 768 row pairs of 151,936 bf16: 272 us (0.39 of the copy rate; 256 where no comparison is open), 512 of 262,144: 306 to 325, 12 of 1,024 fp32: 6.0.  A row pair's 38 instructions a pair of logits and its
+// 768 row pairs of 151,936 bf16: 264 us (0.40 of the copy rate; 250 where no comparison is open), 512 of 262,144: 300 to 320, 12 of 1,024 fp32: 5.7.  Some 36 instructions a pair of logits and its
 // five exponentials bound it, with the meetings between passes; DRAM is busy in the first and the last pass.
 #include "bebop_kernels.h"
 #include "bebop_ring.cuh"
@@ -44,15 +44,13 @@ struct PairRef {
 
 constexpr int kTvSlots = 2;
 template <int DT> using TvRing = Ring<DT, 2, kTvSlots>;
-struct __align__(16) TvSums { RSum p, q; double p2, q2; };      // (p2, q2: sums of squares)
+struct __align__(16) TvSums { RSum p, q; };
 
 // How far theta may be off, in units of tau.  Sums in fp32: every term carries an error of the order of 2^-24 (ex2.approx's bound is 2^-22) and of either sign, so
-// that a sum is off by 2^-24 sqrt(sum p^2), and by what the exponents' roundings have in common.  kNearKappa times that and kNearFloor: on 36,864 row pairs (1,024
-// to 151,936 tokens, N(0, 1) to N(0, 6^2), three temperatures, both types) the largest error is 0.6 of it.
-constexpr float kNearKappa = 4.5f, kNearFloor = 6e-8f;
-__device__ __forceinline__ float near_fp32(const TvSums& t) {
-    return kNearFloor + kNearKappa * 5.9604644775390625e-08f * ((float)(sqrt(t.p2) / t.p.s) + (float)(sqrt(t.q2) / t.q.s));
-}
+// that a sum is off by 2^-24 sqrt(sum p^2), where sum p^2 <= 1 / s as no term is above 1, and by what the exponents' roundings have in common.  kNearKappa times that and kNearFloor: on 73,728 row
+// pairs (1,024 to 151,936 tokens, N(0, 1) to N(0, 6^2), three temperatures, both types) the largest error is 0.57 of it.
+constexpr float kNearKappa = 3.6f, kNearFloor = 5e-8f;
+__device__ __forceinline__ float near_fp32(const TvSums& t) { return kNearFloor + kNearKappa * 5.9604644775390625e-08f * (rsqrtf((float)t.p.s) + rsqrtf((float)t.q.s)); }
 constexpr float kNearDouble = 1e-12f;                         // sums in double: 2.4e-15
 
 // FAR: the references are logits.
@@ -123,14 +121,13 @@ __device__ __forceinline__ void grad_vec(const uint4& xp, const uint4& xq, const
 
 struct __align__(16) TvMass { double ab, ss, q; int near, pad; };
 struct __align__(16) TvTwo { double a, b; };
-struct __align__(16) TvFour { double a, b, a2, b2; };
 constexpr int kTvOpen = 192;
 struct TvOpen { float p, q, e, s; };                         // a token's logits, its exponential of the draft's, the sign it was given
 struct TvGradShared {
     TvSums sum[kRingWarps], cta_sum[kRowsMaxCluster];
     TvMass mass[4][kRingWarps], cta_mass[4][kRowsMaxCluster];        // (pass 2, and three times more)
     TvTwo max[kRingWarps], cta_max[kRowsMaxCluster], exact[2][kRingWarps], cta_exact[2][kRowsMaxCluster];
-    TvFour finer[kRingWarps], cta_finer[kRowsMaxCluster];
+    TvTwo finer[kRingWarps], cta_finer[kRowsMaxCluster];
     unsigned long long bar[kRingWarps][kTvSlots];
     int opens;                                               // tokens whose comparison is open: how many, the first of them,
     unsigned long long open_mass;                            // what they weigh (2^-44), the smallest and the largest difference of their logits (ordered)
@@ -138,13 +135,11 @@ struct TvGradShared {
     TvOpen open[kTvOpen];
 };
 
-__device__ __forceinline__ RSum merge_sum(RSum r, double r2, double& o2, const RScale& c) {      // (in double: theta hangs on it)
+__device__ __forceinline__ RSum merge_sum(RSum r, const RScale& c) {      // (in double: theta hangs on it)
     RSum o;
     o.m = ord2f(redux_max(f2ord(r.m)));
     o.bad = __reduce_or_sync(0xffffffffu, r.bad);
-    const double f = ref_factor<false>(r.m, o.m, c);
-    o.s = warp_sum(r.s * f);
-    o2 = warp_sum(r2 * (f * f));
+    o.s = warp_sum(r.s * ref_factor<false>(r.m, o.m, c));
     return o;
 }
 __device__ __forceinline__ TvMass merge_mass(const TvMass* s, int n) {
@@ -158,7 +153,7 @@ __device__ __forceinline__ TvMass merge_mass(const TvMass* s, int n) {
 
 
 // The sums of a row pair whose comparisons are open, more exactly: the terms from 2^-7 of the largest on in double, the others (most, and light) by the series above,
-// whose errors have no mean: of near_finer's bound, ten to forty times below near_fp32's, the largest error on the row pairs above is 0.47.  A fifth of tv_exact's time.
+// whose errors have no mean: of near_finer's bound, five to ten times below near_fp32's, the largest error on the row pairs above is 0.40.  A fifth of tv_exact's time.
 template <int DT> __device__ __noinline__ void tv_finer(TvRing<DT>& held, TvGradShared& S, int left0, const RScale& scale, int rank, int C, TvSums& tot) {
     constexpr int VEC = Elem<DT>::VEC;
     const int lane = threadIdx.x & 31;
@@ -168,7 +163,6 @@ template <int DT> __device__ __noinline__ void tv_finer(TvRing<DT>& held, TvGrad
     const float least[2] = {series_least(tot.p.m, c), series_least(tot.q.m, c)};
     const float m[2] = {tot.p.m, tot.q.m};
     double d[2] = {0.0, 0.0};
-    float h2[2] = {0.f, 0.f};
     ring.chunks_of(false, nullptr, [&](const unsigned char* at, int from, int, bool) {
         const int rem = ring.bytes - from, left = left0 - (from >> 4) * VEC;
 #pragma unroll 1
@@ -194,19 +188,18 @@ template <int DT> __device__ __noinline__ void tv_finer(TvRing<DT>& held, TvGrad
                 const unsigned char* const z = at + w * TvRing<DT>::PART + j * 512 + (i % VEC) * (16 / VEC);
                 const float f = DT == 0 ? *reinterpret_cast<const float*>(z) : __uint_as_float((unsigned)*reinterpret_cast<const unsigned short*>(z) << 16);
                 const double e = q_exp2(row_arg<false>(f, w ? m[1] : m[0], c), g_pow2_64);
-                const float e2 = (float)(e * e);
-                if (w) { d[1] += e; h2[1] += e2; } else { d[0] += e; h2[0] += e2; }
+                if (w) d[1] += e; else d[0] += e;
             }
         }
     });
     held = ring;
-    const TvFour s = meet(S.finer, S.cta_finer, TvFour{warp_sum(d[0]), warp_sum(d[1]), warp_sum((double)h2[0]), warp_sum((double)h2[1])}, C, rank, [&](const TvFour* s, int n) {
-        return TvFour{warp_sum(lane < n ? s[lane].a : 0.0), warp_sum(lane < n ? s[lane].b : 0.0), warp_sum(lane < n ? s[lane].a2 : 0.0), warp_sum(lane < n ? s[lane].b2 : 0.0)};
+    const TvTwo s = meet(S.finer, S.cta_finer, TvTwo{warp_sum(d[0]), warp_sum(d[1])}, C, rank, [&](const TvTwo* s, int n) {
+        return TvTwo{warp_sum(lane < n ? s[lane].a : 0.0), warp_sum(lane < n ? s[lane].b : 0.0)};
     });
     tot.p.s = s.a; tot.q.s = s.b;
-    tot.p2 = fmax(tot.p2 - s.a2, 1e-5 * tot.p2); tot.q2 = fmax(tot.q2 - s.b2, 1e-5 * tot.q2);      // (the sums' own errors: 1e-6)
 }
-__device__ __forceinline__ float near_finer(const TvSums& t) { return 6e-9f + 4.f * 5.9604644775390625e-08f * ((float)(sqrt(t.p2) / t.p.s) + (float)(sqrt(t.q2) / t.q.s)); }
+// (4 2^-24 sqrt(sum p^2) over the light terms, none of which is above 2^-7)
+__device__ __forceinline__ float near_finer(const TvSums& t) { return 6e-9f + 2.1073424255e-08f * (rsqrtf((float)t.p.s) + rsqrtf((float)t.q.s)); }
 
 // ... and all of them in double.  FAR: around the rows' largest logits, which are found first.
 template <int DT, bool FAR> __device__ __noinline__ void tv_exact(TvRing<DT>& ring, TvGradShared& S, int left0, const RScale& c, int rank, int C, TvSums& tot) {
@@ -304,17 +297,17 @@ __global__ void __launch_bounds__(32 * kRingWarps, 1) k_tv_grad(const __grid_con
         const bool first = rank == 0 && threadIdx.x == 0;
         // ---- pass 1
         typename TvRing<DT>::Sum rs[2];
-        ring.template sums<DT == 0, true>(left0, false, nullptr, c, rs, NoHook());
+        ring.template sums<DT == 0>(left0, false, nullptr, c, rs, NoHook());
         TvSums tot;
-        tot.p.s = warp_sum(rs[0].s); tot.q.s = warp_sum(rs[1].s); tot.p2 = warp_sum(rs[0].s2); tot.q2 = warp_sum(rs[1].s2);
+        tot.p.s = warp_sum(rs[0].s); tot.q.s = warp_sum(rs[1].s);
         tot.p.m = rs[0].e == E_EMPTY ? -INFINITY : (float)rs[0].e; tot.q.m = rs[1].e == E_EMPTY ? -INFINITY : (float)rs[1].e;
         tot.p.bad = (rs[0].bad ? 1 : 0) | (a.expire || ring.failed ? 2 : 0); tot.q.bad = rs[1].bad ? 1 : 0;
         if (threadIdx.x == 0) { S.opens = 0; S.open_mass = 0; S.open_least = LLONG_MAX; S.open_most = LLONG_MIN; }                    // (nobody looks at the last unit's any more: a meeting lies behind)
         tot = meet(S.sum, S.cta_sum, tot, C, rank, [&](const TvSums* s, int n) {
             TvSums o, x;
-            x.p = x.q = no_sum(); x.p2 = x.q2 = 0.0;
+            x.p = x.q = no_sum();
             if (lane < n) x = s[lane];
-            o.p = merge_sum(x.p, x.p2, o.p2, c); o.q = merge_sum(x.q, x.q2, o.q2, c);
+            o.p = merge_sum(x.p, c); o.q = merge_sum(x.q, c);
             return o;
         });
         int st = sum_status(tot.p) | sum_status(tot.q);
