@@ -13,7 +13,7 @@
 //   pass 2  sum |p - q|, S, the smallest |z_p - z_q - theta|
 //   again   where that smallest distance is below the bound: the sums more exactly (33 us of the CTA's time at 151,936 tokens), by which the tokens that were open are decided
 //   pass 3  the gradient
-// 768 row pairs of 151,936 bf16: 264 us (0.40 of the copy rate; 250 where no comparison is open), 512 of 262,144: 300 to 320, 12 of 1,024 fp32: 5.7.  Some 36 instructions a pair of logits and its
+// 768 row pairs of 151,936 bf16: 264 us (0.41 of the copy rate; 241 where no comparison is open, 289 with three), 512 of 262,144: 281 to 341, 12 of 1,024 fp32: 5.6.  Some 36 instructions a pair of logits and its
 // five exponentials bound it, with the meetings between passes; DRAM is busy in the first and the last pass.
 #include "bebop_kernels.h"
 #include "bebop_ring.cuh"
