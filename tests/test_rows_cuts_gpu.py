@@ -149,3 +149,42 @@ def test_draws_next_to_the_border_of_a_token(dtype, V, std):
         assert sure.mean() > 0.95 and (got["accept_len"].cpu().numpy() == 0).all()
         wrong = (got["out_tokens"].cpu().numpy() != ref["out_tokens"]).any(1) & sure
         assert not wrong.any(), np.nonzero(wrong)[0][:5]
+
+
+def test_a_shape_met_first_in_a_capture_and_calls_from_several_threads():
+    """What the host works out for a shape (cuts, how many clusters fit) needs no call before the capture, and no lock."""
+    import threading
+    def calls(V, seed):
+        t, d = rows((37,), V, "bf16", seed), rows((37,), V, "bf16", seed + 1)
+        _, ids, top, lse = teacher(37, V, 11, "bf16", seed + 2)
+        x = rows((5, 3), V, "bf16", seed + 3)
+        tok = x[:, :2].float().argmax(2).int()
+        ua, uf = uniform((5, 2), seed + 4), uniform((5,), seed + 5)
+        return [lambda: P.bebop_tv_grad(t, d), lambda: P.bebop_distill(d, ids, top, target_lse=lse), lambda: P.bebop_target_only_verify(x, tok, ua, uf)]
+    for f in calls(23456, 330):
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            kept = f()
+        graph.replay()
+        torch.cuda.synchronize()
+        want = f()
+        assert all((kept[k] is None and want[k] is None) or torch.equal(kept[k], want[k]) for k in want)
+    jobs = [(calls(V, V), [None] * 3) for V in (1111, 5555, 23457, 44444)]
+    torch.cuda.synchronize()
+
+    def work(fs, out):
+        with torch.cuda.stream(torch.cuda.Stream()):
+            for _ in range(20):
+                for i, f in enumerate(fs):
+                    out[i] = f()
+            torch.cuda.current_stream().synchronize()
+    threads = [threading.Thread(target=work, args=j) for j in jobs]
+    for th in threads:
+        th.start()
+    for th in threads:
+        th.join()
+    for fs, out in jobs:
+        for f, got in zip(fs, out):
+            want = f()
+            assert all((got[k] is None and want[k] is None) or torch.equal(got[k], want[k]) for k in want)
